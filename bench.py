@@ -60,7 +60,8 @@ def decode_source_digest() -> str:
     """Of the decode kernels' source without comments and white space: tells whether recorded counters are of this code."""
     import hashlib
     import re
-    text = open(os.path.join(ROOT, "paper_2504_09936_amd", "csrc", "decode_attn.hip")).read()
+    files = [os.path.join(ROOT, "paper_2504_09936_amd", "csrc", f) for f in ("decode_common.hpp", "decode_attn.hip")]
+    text = "".join(open(f).read() for f in files if os.path.exists(f))
     text = re.sub(r"\s+", "", re.sub(r"//[^\n]*|/\*.*?\*/", "", text, flags=re.S))
     return hashlib.sha256(text.encode()).hexdigest()[:12]
 
