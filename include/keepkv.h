@@ -289,6 +289,67 @@ keepkv_status keepkv_prefill_merge(const keepkv_layout *layout, const keepkv_cac
                                    keepkv_cache *dst, const int32_t *near, float alpha,
                                    void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- Caches held in 8 bits -----------------------------------------------------------------------------------
+ * A cache of codes: K and V as OCP e4m3 values (8 bits: 4 significant bits, largest 448, no infinity) times one scale for each block
+ * of KEEPKV_QUANT_BLOCK consecutive slots of a (batch, kv head), K and V apart:  value = code * scale of the slot's block.
+ * With a the largest finite magnitude of the block's live rows the scale is the smallest power of two 2^e for which
+ * a <= 448 * 2^e, -110 <= e <= 120, and a code is the row's element / scale rounded to nearest even; an element that is not
+ * finite becomes NaN.  Since a scale is a power of two, dividing by it rounds nothing, reading back is exact (in f32 and in
+ * bf16), and rows that were read back are quantised again to the same values except where those become subnormal under a
+ * larger scale (a value below 2^-6 of the scale keeps multiples of 2^-9 of it).
+ * Half the bytes of a bf16 cache, and its decode calls read them as they are. */
+#define KEEPKV_QUANT_BLOCK 32
+
+/* One layer's cache of codes (HOST struct of DEVICE pointers, caller-owned).  The calls that read no rows take &cache->c as their
+ * cache: keepkv_score, keepkv_select, keepkv_select_by_key, keepkv_select_aged.  All others would take the codes for
+ * rows of the layout's dtype: give them a cache that keepkv_dequantize has written. */
+typedef struct {
+  keepkv_cache c;       /* as described there, but k, v: DEVICE uint8 [B, Hkv, capacity, D] e4m3 codes;  */
+                        /* plan_wavefronts 0, 4 or 8                                                    */
+  float *k_scale;       /* [B, Hkv, ceil(capacity / KEEPKV_QUANT_BLOCK)] scale of each block of K codes;  */
+  float *v_scale;       /* and of V codes.  Those of blocks without a live slot mean nothing             */
+} keepkv_quant_cache;
+
+/* Quantise a cache: the live slots of src (rows of the layout's dtype) into codes of dst, with their votes, log_s and born, and
+ * t_obs and len.  Dead slots of dst and scales of blocks without a live slot are left as they are.  src and dst must not
+ * overlap; dst->c.capacity >= src->capacity.  Needs no workspace. */
+keepkv_status keepkv_quantize(const keepkv_layout *layout, const keepkv_cache *src,
+                              keepkv_quant_cache *dst, void *stream);
+
+/* Read a cache of codes back: the live slots of src as rows of the layout's dtype in dst, with votes, log_s, born, t_obs and len.
+ * Dead slots of dst are left as they are.  src and dst must not overlap; dst->capacity >= src->c.capacity.  Needs no workspace. */
+keepkv_status keepkv_dequantize(const keepkv_layout *layout, const keepkv_quant_cache *src,
+                                keepkv_cache *dst, void *stream);
+
+/* keepkv_append on a cache of codes, for one token or several: of k_t, v_t [B, Hkv, n_tokens, D] DEVICE (layout dtype) the first
+ * counts[b,h] rows (DEVICE int32 [B, Hkv], clamped to 0 .. n_tokens; NULL: all n_tokens) join head (b, h) as slots len[b,h], ... with
+ * votes = 1, log_s = -inf, born = t_obs[b,h], as many as its capacity holds, and len grows by their number;
+ * `overflow` (DEVICE int32, may be NULL) is set to 1 if some did not fit.  A block that held live slots before keeps its scale unless
+ * the new rows need a larger one, s' : then its live codes become rne(code * s / s'), a shift of exponents that is exact
+ * except where a code becomes subnormal.  A block whose first slot is among the new ones starts with the scale that they need.
+ * n_tokens >= 1.  Needs no workspace. */
+keepkv_status keepkv_append_quant(const keepkv_layout *layout, keepkv_quant_cache *cache,
+                                  const void *k_t, const void *v_t, int32_t n_tokens,
+                                  const int32_t *counts, int32_t *overflow, void *stream);
+
+/* keepkv_decode_attn on a cache of codes: Eq. 6 over the values code * scale, with the same arguments (q and out in the layout's
+ * dtype, f32 or bf16) and the same treatment of empty and dead slots.  Products of q and codes are exact, sums f32. */
+keepkv_status keepkv_decode_attn_quant(const keepkv_layout *layout, const keepkv_quant_cache *cache,
+                                       const void *q, void *out, float *logits_out, float *lse_out,
+                                       void *workspace, size_t workspace_bytes, void *stream);
+
+/* keepkv_decode_step on a cache of codes: keepkv_append_quant of one token, keepkv_decode_attn_quant over the grown cache,
+ * keepkv_score with its logits.  The new token is attended as its codes say. */
+keepkv_status keepkv_decode_step_quant(const keepkv_layout *layout, keepkv_quant_cache *cache, const void *q,
+                                       const void *k_t, const void *v_t, void *out, float *logits_out,
+                                       float alpha, int32_t *overflow, void *workspace,
+                                       size_t workspace_bytes, void *stream);
+
+/* keepkv_decode_plan for the two calls above (their plans differ, a slot being half the bytes).  keepkv_workspace_bytes covers
+ * them; a plan forced by plan_slots_per_split needs the bytes given there. */
+keepkv_status keepkv_decode_plan_quant(const keepkv_layout *layout, int32_t capacity, int32_t *n_split,
+                                       int32_t *slots_per_split, int32_t *wavefronts);
+
 /* Measurement probes (not part of the method): what the GPU sustains, to set next to the
  * published peaks.  keepkv_probe_read: `n_workgroups` workgroups stream `bytes` (a multiple of
  * 16) of DEVICE memory at `src` once with coalesced 16-byte loads; nothing is written except

@@ -38,6 +38,10 @@ class _Cache(C.Structure):
                 ("plan_slots_per_split", C.c_int32), ("plan_wavefronts", C.c_int32)]
 
 
+class _QuantCache(C.Structure):
+    _fields_ = [("c", _Cache), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
 _P = C.c_void_p
 _lib.keepkv_strerror.restype = C.c_char_p
 _lib.keepkv_strerror.argtypes = [C.c_int]
@@ -69,9 +73,17 @@ _lib.keepkv_prefill_merge.argtypes = [C.POINTER(_Layout), C.POINTER(_Cache), C.P
                                       C.c_size_t, _P]
 _lib.keepkv_probe_read.argtypes = [_P, C.c_size_t, C.c_int32, _P, _P]
 _lib.keepkv_probe_mfma.argtypes = [C.c_int32, C.c_int32, C.c_int32, _P, C.POINTER(C.c_double), _P]
+_lib.keepkv_quantize.argtypes = [C.POINTER(_Layout), C.POINTER(_Cache), C.POINTER(_QuantCache), _P]
+_lib.keepkv_dequantize.argtypes = [C.POINTER(_Layout), C.POINTER(_QuantCache), C.POINTER(_Cache), _P]
+_lib.keepkv_append_quant.argtypes = [C.POINTER(_Layout), C.POINTER(_QuantCache), _P, _P, C.c_int32, _P, _P, _P]
+_lib.keepkv_decode_attn_quant.argtypes = [C.POINTER(_Layout), C.POINTER(_QuantCache), _P, _P, _P, _P, _P, C.c_size_t, _P]
+_lib.keepkv_decode_step_quant.argtypes = [C.POINTER(_Layout), C.POINTER(_QuantCache), _P, _P, _P, _P, _P, C.c_float, _P, _P,
+                                          C.c_size_t, _P]
+_lib.keepkv_decode_plan_quant.argtypes = [C.POINTER(_Layout), C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_int32),
+                                          C.POINTER(C.c_int32)]
 _lib.keepkv_decode_plan.argtypes = [C.POINTER(_Layout), C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_int32),
                                     C.POINTER(C.c_int32)]
-for _f in ("select_aged", "merge_inplace", "prefill_match", "prefill_merge", "decode_step_static", "decode_plan", "probe_read", "probe_mfma", "append", "decode_attn", "decode_step", "workspace_init", "score", "score_window", "select",
+for _f in ("quantize", "dequantize", "append_quant", "decode_attn_quant", "decode_step_quant", "decode_plan_quant", "select_aged", "merge_inplace", "prefill_match", "prefill_merge", "decode_step_static", "decode_plan", "probe_read", "probe_mfma", "append", "decode_attn", "decode_step", "workspace_init", "score", "score_window", "select",
            "select_by_key", "match",
            "merge"):
     getattr(_lib, "keepkv_" + _f).restype = C.c_int
@@ -79,7 +91,8 @@ for _f in ("select_aged", "merge_inplace", "prefill_match", "prefill_merge", "de
 EXPORTS = ["keepkv_strerror", "keepkv_version", "keepkv_workspace_bytes", "keepkv_workspace_init", "keepkv_decode_plan",
            "keepkv_append", "keepkv_decode_attn", "keepkv_decode_step", "keepkv_decode_step_static", "keepkv_score", "keepkv_score_window", "keepkv_select",
            "keepkv_select_by_key", "keepkv_select_aged", "keepkv_match", "keepkv_merge", "keepkv_merge_inplace", "keepkv_prefill_match", "keepkv_prefill_merge",
-           "keepkv_probe_read", "keepkv_probe_mfma"]
+           "keepkv_quantize", "keepkv_dequantize", "keepkv_append_quant", "keepkv_decode_attn_quant", "keepkv_decode_step_quant",
+           "keepkv_decode_plan_quant", "keepkv_probe_read", "keepkv_probe_mfma"]
 
 
 class KeepKVError(RuntimeError):
@@ -146,24 +159,8 @@ class Layout:
         return torch.bfloat16 if self.dtype == BF16 else torch.float32
 
 
-class Cache:
-    """One layer's cache as device tensors (plain storage; no arithmetic happens here)."""
-
-    def __init__(self, layout: Layout, capacity: int, device="cuda"):
-        B, H, D = layout.batch, layout.n_kv_heads, layout.head_dim
-        self.layout, self.capacity = layout, capacity
-        self.len_hint = 0     # host-side upper bound on len (0 = unknown); see keepkv_cache.len_hint
-        self.plan_slots_per_split = 0   # decode launch overrides (0 = automatic); see keepkv_cache
-        self.plan_wavefronts = 0
-        self.k = torch.zeros(B, H, capacity, D, dtype=layout.torch_dtype, device=device)
-        self.v = torch.zeros(B, H, capacity, D, dtype=layout.torch_dtype, device=device)
-        self.votes = torch.zeros(B, H, capacity, dtype=torch.int32, device=device)
-        self.log_s = torch.full((B, H, capacity), float("-inf"), dtype=torch.float32, device=device)
-        self.born = torch.zeros(B, H, capacity, dtype=torch.int32, device=device)
-        self.t_obs = torch.zeros(B, H, dtype=torch.int32, device=device)
-        self.len = torch.zeros(B, H, dtype=torch.int32, device=device)
-
-    FIELDS = ("k", "v", "votes", "log_s", "born", "t_obs", "len")
+class _Saved:
+    """Dumps and replays of a cache: its FIELDS and capacity."""
 
     def state(self) -> dict:
         """Host copies of every array of the cache (for dumps and replays of a failing step; plain copies)."""
@@ -187,10 +184,78 @@ class Cache:
     def load(self, path: str) -> None:
         self.load_state(torch.load(path, map_location="cpu", weights_only=True))
 
+
+class Cache(_Saved):
+    """One layer's cache as device tensors (plain storage; no arithmetic happens here)."""
+
+    def __init__(self, layout: Layout, capacity: int, device="cuda"):
+        B, H, D = layout.batch, layout.n_kv_heads, layout.head_dim
+        self.layout, self.capacity = layout, capacity
+        self.len_hint = 0     # host-side upper bound on len (0 = unknown); see keepkv_cache.len_hint
+        self.plan_slots_per_split = 0   # decode launch overrides (0 = automatic); see keepkv_cache
+        self.plan_wavefronts = 0
+        self.k = torch.zeros(B, H, capacity, D, dtype=layout.torch_dtype, device=device)
+        self.v = torch.zeros(B, H, capacity, D, dtype=layout.torch_dtype, device=device)
+        self.votes = torch.zeros(B, H, capacity, dtype=torch.int32, device=device)
+        self.log_s = torch.full((B, H, capacity), float("-inf"), dtype=torch.float32, device=device)
+        self.born = torch.zeros(B, H, capacity, dtype=torch.int32, device=device)
+        self.t_obs = torch.zeros(B, H, dtype=torch.int32, device=device)
+        self.len = torch.zeros(B, H, dtype=torch.int32, device=device)
+
+    FIELDS = ("k", "v", "votes", "log_s", "born", "t_obs", "len")
+
     def c(self) -> _Cache:
         return _Cache(self.k.data_ptr(), self.v.data_ptr(), self.votes.data_ptr(), self.log_s.data_ptr(),
                       self.born.data_ptr(), self.t_obs.data_ptr(), self.len.data_ptr(), self.capacity, int(self.len_hint),
                       int(self.plan_slots_per_split), int(self.plan_wavefronts))
+
+
+QUANT_BLOCK = 32      # slots that share a scale (KEEPKV_QUANT_BLOCK)
+
+
+class QuantCache(_Saved):
+    """One layer's cache held in 8 bits: e4m3 codes with a scale per block of QUANT_BLOCK slots and head, as device tensors.
+    score, select, select_by_key and select_aged, which read no rows, take it as they take a Cache; the other calls on rows of the
+    layout's dtype refuse it (dequantize first)."""
+
+    def __init__(self, layout: Layout, capacity: int, device="cuda"):
+        B, H, D = layout.batch, layout.n_kv_heads, layout.head_dim
+        self.layout, self.capacity = layout, capacity
+        self.len_hint = 0     # as in Cache
+        self.plan_slots_per_split = 0
+        self.plan_wavefronts = 0
+        codes, blocks = (B, H, capacity, D), (B, H, -(-capacity // QUANT_BLOCK))
+        self.k = torch.zeros(codes, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
+        self.v = torch.zeros(codes, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
+        self.k_scale = torch.ones(blocks, dtype=torch.float32, device=device)
+        self.v_scale = torch.ones(blocks, dtype=torch.float32, device=device)
+        self.votes = torch.zeros(B, H, capacity, dtype=torch.int32, device=device)
+        self.log_s = torch.full((B, H, capacity), float("-inf"), dtype=torch.float32, device=device)
+        self.born = torch.zeros(B, H, capacity, dtype=torch.int32, device=device)
+        self.t_obs = torch.zeros(B, H, dtype=torch.int32, device=device)
+        self.len = torch.zeros(B, H, dtype=torch.int32, device=device)
+
+    FIELDS = ("k", "v", "k_scale", "v_scale", "votes", "log_s", "born", "t_obs", "len")
+
+    def c(self):
+        raise TypeError("this call reads rows of the layout's dtype, a QuantCache holds codes: dequantize it into a Cache")
+
+    def state_c(self) -> _Cache:
+        return Cache.c(self)
+
+    def quant_c(self) -> _QuantCache:
+        return _QuantCache(Cache.c(self), self.k_scale.data_ptr(), self.v_scale.data_ptr())
+
+
+def _quant(cache) -> _QuantCache:
+    if not isinstance(cache, QuantCache):
+        raise TypeError("a QuantCache is expected, not a " + type(cache).__name__)
+    return cache.quant_c()
+
+
+def _state(cache) -> _Cache:
+    """For the calls that read no rows."""
+    return cache.state_c() if isinstance(cache, QuantCache) else cache.c()
 
 
 def version() -> int:
@@ -247,7 +312,7 @@ def decode_attn(layout: Layout, cache: Cache, q, out, logits_out, lse_out, works
 def score(layout: Layout, cache: Cache, logits, alpha: float) -> None:
     fast = _fast_call("score", layout, cache)
     _check(fast(layout, cache, logits, alpha) if fast else
-           _lib.keepkv_score(C.byref(layout.c()), C.byref(cache.c()), _ptr(logits), alpha, _stream()), "keepkv_score")
+           _lib.keepkv_score(C.byref(layout.c()), C.byref(_state(cache)), _ptr(logits), alpha, _stream()), "keepkv_score")
 
 
 def score_window(layout: Layout, cache: Cache, q_win, window: int, alpha: float, first_pos: int = -1) -> None:
@@ -257,7 +322,7 @@ def score_window(layout: Layout, cache: Cache, q_win, window: int, alpha: float,
 
 def select(layout: Layout, cache: Cache, budget: int, n_sink: int, n_recent: int, alpha: float,
            keep_idx, evict_idx, n_evict, workspace) -> None:
-    _check(_lib.keepkv_select(C.byref(layout.c()), C.byref(cache.c()), budget, n_sink, n_recent, alpha,
+    _check(_lib.keepkv_select(C.byref(layout.c()), C.byref(_state(cache)), budget, n_sink, n_recent, alpha,
                               _ptr(keep_idx), _ptr(evict_idx), _ptr(n_evict), _ptr(workspace),
                               0 if workspace is None else workspace.numel() * workspace.element_size(),
                               _stream()), "keepkv_select")
@@ -273,9 +338,42 @@ def decode_plan(layout: Layout, capacity: int):
 
 def select_by_key(layout: Layout, cache: Cache, rank, budget: int, n_sink: int, n_recent: int,
                   keep_idx, evict_idx, n_evict, workspace) -> None:
-    _check(_lib.keepkv_select_by_key(C.byref(layout.c()), C.byref(cache.c()), _ptr(rank), budget, n_sink, n_recent,
+    _check(_lib.keepkv_select_by_key(C.byref(layout.c()), C.byref(_state(cache)), _ptr(rank), budget, n_sink, n_recent,
                                      _ptr(keep_idx), _ptr(evict_idx), _ptr(n_evict), _ptr(workspace),
                                      _nbytes(workspace), _stream()), "keepkv_select_by_key")
+
+
+def quantize(layout: Layout, src: Cache, dst: QuantCache) -> None:
+    _check(_lib.keepkv_quantize(C.byref(layout.c()), C.byref(src.c()), C.byref(_quant(dst)), _stream()), "keepkv_quantize")
+
+
+def dequantize(layout: Layout, src: QuantCache, dst: Cache) -> None:
+    _check(_lib.keepkv_dequantize(C.byref(layout.c()), C.byref(_quant(src)), C.byref(dst.c()), _stream()), "keepkv_dequantize")
+
+
+def append_quant(layout: Layout, cache: QuantCache, k_t, v_t, n_tokens: int = 1, counts=None, overflow=None) -> None:
+    _check(_lib.keepkv_append_quant(C.byref(layout.c()), C.byref(_quant(cache)), _ptr(k_t), _ptr(v_t), n_tokens, _ptr(counts),
+                                    _ptr(overflow), _stream()), "keepkv_append_quant")
+
+
+def decode_attn_quant(layout: Layout, cache: QuantCache, q, out, logits_out, lse_out, workspace) -> None:
+    _check(_lib.keepkv_decode_attn_quant(C.byref(layout.c()), C.byref(_quant(cache)), _ptr(q), _ptr(out), _ptr(logits_out),
+                                         _ptr(lse_out), _ptr(workspace), _nbytes(workspace), _stream()),
+           "keepkv_decode_attn_quant")
+
+
+def decode_step_quant(layout: Layout, cache: QuantCache, q, k_t, v_t, out, logits_out, alpha: float, overflow, workspace) -> None:
+    _check(_lib.keepkv_decode_step_quant(C.byref(layout.c()), C.byref(_quant(cache)), _ptr(q), _ptr(k_t), _ptr(v_t), _ptr(out),
+                                         _ptr(logits_out), alpha, _ptr(overflow), _ptr(workspace), _nbytes(workspace),
+                                         _stream()), "keepkv_decode_step_quant")
+
+
+def decode_plan_quant(layout: Layout, capacity: int):
+    """decode_plan for the decode calls on a QuantCache."""
+    ns, per, wv = C.c_int32(0), C.c_int32(0), C.c_int32(0)
+    _check(_lib.keepkv_decode_plan_quant(C.byref(layout.c()), capacity, C.byref(ns), C.byref(per), C.byref(wv)),
+           "keepkv_decode_plan_quant")
+    return ns.value, per.value, wv.value
 
 
 def probe_read(src, n_workgroups: int, sink) -> None:
@@ -299,7 +397,7 @@ def match(layout: Layout, cache: Cache, budget: int, keep_idx, evict_idx, n_evic
 
 def select_aged(layout: Layout, cache: Cache, order, budget: int, n_sink: int, n_recent: int, alpha: float,
                 keep_idx, evict_idx, n_evict, workspace) -> None:
-    _check(_lib.keepkv_select_aged(C.byref(layout.c()), C.byref(cache.c()), _ptr(order), budget, n_sink, n_recent, alpha,
+    _check(_lib.keepkv_select_aged(C.byref(layout.c()), C.byref(_state(cache)), _ptr(order), budget, n_sink, n_recent, alpha,
                                    _ptr(keep_idx), _ptr(evict_idx), _ptr(n_evict), _ptr(workspace), _nbytes(workspace),
                                    _stream()), "keepkv_select_aged")
 
