@@ -339,18 +339,6 @@ constexpr int mfma_stage_bytes(int D, int G) { return (G * D * 2 + 1023) / 1024 
 // is part of the statement.
 typedef __attribute__((ext_vector_type(4))) int i32x4_t;
 
-template <int G>
-__device__ __forceinline__ float head_sum(float x) {   // sum over the G heads held by G consecutive lanes
-  if constexpr (G >= 2) x += dpp_f32<0xB1>(x);          // quad_perm [1,0,3,2]
-  if constexpr (G >= 4) x += dpp_f32<0x4E>(x);          // quad_perm [2,3,0,1]
-  if constexpr (G >= 8) x += dpp_f32<0x141>(x);         // row_half_mirror
-  return x;
-}
-
-__device__ __forceinline__ uint32_t pack_hi16(float lo_elem, float hi_elem) {   // {bf16 trunc(lo_elem), bf16 trunc(hi_elem)}
-  return (__builtin_bit_cast(uint32_t, lo_elem) >> 16) | (__builtin_bit_cast(uint32_t, hi_elem) & 0xFFFF0000u);
-}
-
 // The vector ALU's share.  A SIMD has two of these wavefronts and issues one 64-lane instruction in four cycles, so what a
 // tile costs beyond its loads is its instruction count: with every lane working out all 8 slots of its column (16 / G
 // lanes then do the same work) a tile took 430 instructions, 0.8 us alone and 1.6 us beside a second wavefront, most of
@@ -624,22 +612,7 @@ __global__ __launch_bounds__(kMfmaWaves* kWave, 2) void decode_mfma_kernel(Decod
     }
     // ---- this lane's NV values of the column
     float sv[NV];
-    if constexpr (NV == 4) {
-#pragma unroll
-      for (int v = 0; v < 4; ++v) sv[v] = (r_l & 1) ? s[1][v] : s[0][v];
-    } else if constexpr (NV == 2) {
-#pragma unroll
-      for (int v = 0; v < 2; ++v) {
-        const float t0 = (r_l & 1) ? s[0][2 + v] : s[0][v], t1 = (r_l & 1) ? s[1][2 + v] : s[1][v];
-        sv[v] = (r_l & 2) ? t1 : t0;
-      }
-    } else {
-      float t[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) t[j] = (pos0 & 1) ? s[j >> 1][2 * (j & 1) + 1] : s[j >> 1][2 * (j & 1)];
-      const float u0 = (pos0 & 2) ? t[1] : t[0], u1 = (pos0 & 2) ? t[3] : t[2];
-      sv[0] = (pos0 & 4) ? u1 : u0;
-    }
+    take_shares<G>(s, r_l, pos0, sv);
     // ---- logits (log2 domain, log2(votes) folded in), group-mean logit for the EMA
     float z[NV], xm[NV], lp[NV];
     if constexpr (NV == 1) lp[0] = lp_lane;
@@ -669,17 +642,8 @@ __global__ __launch_bounds__(kMfmaWaves* kWave, 2) void decode_mfma_kernel(Decod
     }
     l_run = fmaf(l_run, c, ps);
     m_run = mn;
-    if (!first && __any(c != 1.f)) {             // uniform: rescale the accumulators, row r = head r mod G
-                                                 // (with ONE only the extra tile of the appended token gets here)
-      const float c_other = dpp_f32<0x124>(c);   // G = 8: of the head four further (every lane reads: not inside the choice)
-      const float cq = G < 8 || ((l16 >> 2) & 1) == (q & 1) ? c : c_other;
-      const float ci[4] = {dpp_f32<0x00>(cq), dpp_f32<G == 1 ? 0x00 : 0x55>(cq), dpp_f32<G <= 2 ? 0x00 : 0xAA>(cq),
-                           dpp_f32<G == 1 ? 0x00 : G == 2 ? 0x55 : 0xFF>(cq)};
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int nt = 0; nt < NTILE; ++nt) O[nt][i] *= ci[i];
-    }
+    if (!first && __any(c != 1.f))               // uniform (with ONE only the extra tile of the appended token gets here)
+      rescale_rows<G>(O, c, l16, q);
     first = false;
     if constexpr (kVWait >= 0) {                 // before any store is issued
       // (tied to the softmax sum, so that the wait is not scheduled ahead of the arithmetic it is meant to hide)
@@ -687,36 +651,9 @@ __global__ __launch_bounds__(kMfmaWaves* kWave, 2) void decode_mfma_kernel(Decod
       if (last) look();
       clear_masked_v();
     }
-    // ---- O += P V with P = hi + lo in bf16.  The places of the slots that other lanes took hold the smallest normal
-    // number and not zero: against any finite V it vanishes beside the head's largest weight (1), and an infinity in V
-    // stays one, where zero would make it a NaN.
-    constexpr uint32_t kNone = 0x00800080u;
+    // ---- O += P V with P = hi + lo in bf16
     uint32_t ah[4], al[4];
-    if constexpr (NV == 1) {
-      const uint32_t hb = __builtin_bit_cast(uint32_t, pr[0]) & 0xFFFF0000u;
-      const uint32_t lb = __builtin_bit_cast(uint32_t, pr[0] - __builtin_bit_cast(float, hb)) & 0xFFFF0000u;
-      const uint32_t wh = (pos0 & 1) ? hb | (kNone & 0xFFFFu) : hb >> 16 | (kNone & 0xFFFF0000u);
-      const uint32_t wl = (pos0 & 1) ? lb | (kNone & 0xFFFFu) : lb >> 16 | (kNone & 0xFFFF0000u);
-#pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        ah[d] = (pos0 >> 1) == d && (G > 1 || r_l < 8) ? wh : kNone;
-        al[d] = (pos0 >> 1) == d && (G > 1 || r_l < 8) ? wl : kNone;
-      }
-    } else {
-      constexpr int NW = NV / 2;
-#pragma unroll
-      for (int j = 0; j < NW; ++j) {
-        const float p0 = pr[2 * j], p1 = pr[2 * j + 1];
-        const float l0 = p0 - __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, p0) & 0xFFFF0000u);
-        const float l1 = p1 - __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, p1) & 0xFFFF0000u);
-        const uint32_t wh = pack_hi16(p0, p1), wl = pack_hi16(l0, l1);
-#pragma unroll
-        for (int d = j; d < 4; d += NW) {        // dword d holds the places 2 d, 2 d + 1
-          ah[d] = r_l == d / NW ? wh : kNone;
-          al[d] = r_l == d / NW ? wl : kNone;
-        }
-      }
-    }
+    weights_operand<G, false>(pr, r_l, pos0, ah, al);
     const bf16x8_t a_hi = __builtin_bit_cast(bf16x8_t, make_uint4(ah[0], ah[1], ah[2], ah[3]));
     const bf16x8_t a_lo = __builtin_bit_cast(bf16x8_t, make_uint4(al[0], al[1], al[2], al[3]));
     // transpose read: lane s of a 16-lane block supplies the address of row s / 4, columns 4 (s mod 4) .. + 3, and
@@ -908,52 +845,10 @@ __global__ __launch_bounds__(kMfmaWaves* kWave, 2) void decode_mfma_kernel(Decod
   // the lane (G <= 2), then over the lane halves and (G <= 4) the rows of 16 lanes; each exchange pairs two channel
   // tiles, so the lanes end up with different channel tiles and the LDS stores are wide.
   const float l_tot = over_head_lanes<G>(l_run, [](float a, float b) { return a + b; });
-  constexpr int NH = G < 4 ? G : 4;              // heads per lane
-  float o[NTILE][NH];
-#pragma unroll
-  for (int nt = 0; nt < NTILE; ++nt)
-#pragma unroll
-    for (int h = 0; h < NH; ++h) {
-      if constexpr (G == 1) o[nt][h] = (O[nt][0] + O[nt][1]) + (O[nt][2] + O[nt][3]);
-      else if constexpr (G == 2) o[nt][h] = O[nt][h] + O[nt][h + 2];
-      else o[nt][h] = O[nt][h];
-    }
-#pragma unroll
-  for (int nt = 0; nt < NTILE / 2; ++nt)
-#pragma unroll
-    for (int h = 0; h < NH; ++h) {
-      swap_halves(o[nt][h], o[nt + NTILE / 2][h]);
-      o[nt][h] += o[nt + NTILE / 2][h];
-    }
-  constexpr int NO = G <= 4 ? NTILE / 4 : NTILE / 2;   // channel tiles per lane
-  if constexpr (G <= 4) {
-#pragma unroll
-    for (int nt = 0; nt < NO; ++nt)
-#pragma unroll
-      for (int h = 0; h < NH; ++h) {
-        swap_rows(o[nt][h], o[nt + NO][h]);
-        o[nt][h] += o[nt + NO][h];
-      }
-  }
   constexpr int kPartStride = 2 * TILE_BYTES / (int)sizeof(float);     // floats between the wavefronts' deposits
   float* s_acc = reinterpret_cast<float*>(smem_tiles);                 // [kParts] x [D][G]
   float* s_ml = s_acc + G * D;                                         // [kParts] x ([G] maxima, [G] sums)
-  {
-    float* acc_mine = s_acc + wave * kPartStride;
-    const int nt0 = (NTILE / 2) * (q >> 1) + (G <= 4 ? NO * (q & 1) : 0);
-    const int h0 = G == 8 ? 4 * (q & 1) : 0;
-#pragma unroll
-    for (int nt = 0; nt < NO; ++nt) {
-      float* at = acc_mine + (16 * (nt0 + nt) + l16) * G + h0;
-      if constexpr (NH == 4) *reinterpret_cast<float4*>(at) = make_float4(o[nt][0], o[nt][1], o[nt][2], o[nt][3]);
-      else if constexpr (NH == 2) *reinterpret_cast<float2*>(at) = make_float2(o[nt][0], o[nt][1]);
-      else *at = o[nt][0];
-    }
-    if (q == 0 && l16 < G) {
-      s_ml[wave * kPartStride + l16] = m_run;
-      s_ml[wave * kPartStride + G + l16] = l_tot;
-    }
-  }
+  deposit_state<D, G>(O, m_run, l_tot, s_acc + wave * kPartStride, s_ml + wave * kPartStride, lane);
   if (threadIdx.x == 0) {
     look();                                      // (a wavefront without a tile)
     s_one_xcd = kMayShareXcd && all_on_this_xcd(p, unit, seen);

@@ -183,6 +183,144 @@ __device__ __forceinline__ bool all_on_this_xcd(const DecodeParams& p, int unit,
   return v == here;
 }
 
+template <int G>
+__device__ __forceinline__ float head_sum(float x) {   // sum over the G heads held by G consecutive lanes
+  if constexpr (G >= 2) x += dpp_f32<0xB1>(x);          // quad_perm [1,0,3,2]
+  if constexpr (G >= 4) x += dpp_f32<0x4E>(x);          // quad_perm [2,3,0,1]
+  if constexpr (G >= 8) x += dpp_f32<0x141>(x);         // row_half_mirror
+  return x;
+}
+
+__device__ __forceinline__ uint32_t pack_hi16(float lo_elem, float hi_elem) {   // {bf16 trunc(lo_elem), bf16 trunc(hi_elem)}
+  return (__builtin_bit_cast(uint32_t, lo_elem) >> 16) | (__builtin_bit_cast(uint32_t, hi_elem) & 0xFFFF0000u);
+}
+
+// ---- the two products of a 32-slot tile on 16x16x32 MFMA (bf16 operands, f32 sums) -----------------------------------------
+// Scores come transposed, S^T = K Q^T: column c of lane (c, q) is head c mod G, and its 8 values are the slots
+// 16 st + 4 q + i, i = 0 .. 3, in s[st][i].  The 16 / G lanes of a head share them: lane share r = c / G takes NV of the 8, from place
+// pos0 on.  (NV = 1 for G <= 2: eight shares; of G = 1 the other eight have none.)
+template <int G>
+constexpr int kShare = G >= 2 ? G / 2 : 1;
+
+template <int G>
+__device__ __forceinline__ void take_shares(const f32x4_t (&s)[2], int r_l, int pos0, float (&sv)[kShare<G>]) {
+  constexpr int NV = kShare<G>;
+  if constexpr (NV == 4) {
+#pragma unroll
+    for (int v = 0; v < 4; ++v) sv[v] = (r_l & 1) ? s[1][v] : s[0][v];
+  } else if constexpr (NV == 2) {
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+      const float t0 = (r_l & 1) ? s[0][2 + v] : s[0][v], t1 = (r_l & 1) ? s[1][2 + v] : s[1][v];
+      sv[v] = (r_l & 2) ? t1 : t0;
+    }
+  } else {
+    float t[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) t[j] = (pos0 & 1) ? s[j >> 1][2 * (j & 1) + 1] : s[j >> 1][2 * (j & 1)];
+    const float u0 = (pos0 & 2) ? t[1] : t[0], u1 = (pos0 & 2) ? t[3] : t[2];
+    sv[0] = (pos0 & 4) ? u1 : u0;
+  }
+}
+
+// The weights of a lane share as the A operand of O = P V, hi + lo in bf16 (16 significant bits).  The places of the slots that
+// other lanes took hold the smallest normal number and not zero: against any finite V it vanishes beside the head's largest weight (1),
+// and an infinity in V stays one, where zero would make it a NaN.  Each term is cut off (together within 2^-15 of the weight) or,
+// kNearest, rounded (2^-18).
+template <int G, bool kNearest>
+__device__ __forceinline__ void weights_operand(const float (&pr)[kShare<G>], int r_l, int pos0, uint32_t (&ah)[4], uint32_t (&al)[4]) {
+  constexpr int NV = kShare<G>;
+  constexpr uint32_t kNone = 0x00800080u;
+  if constexpr (NV == 1) {
+    const uint32_t hb = kNearest ? f32_to_bf16_bits(pr[0]) << 16 : __builtin_bit_cast(uint32_t, pr[0]) & 0xFFFF0000u;
+    const float rest = pr[0] - __builtin_bit_cast(float, hb);
+    const uint32_t lb = kNearest ? f32_to_bf16_bits(rest) << 16 : __builtin_bit_cast(uint32_t, rest) & 0xFFFF0000u;
+    const uint32_t wh = (pos0 & 1) ? hb | (kNone & 0xFFFFu) : hb >> 16 | (kNone & 0xFFFF0000u);
+    const uint32_t wl = (pos0 & 1) ? lb | (kNone & 0xFFFFu) : lb >> 16 | (kNone & 0xFFFF0000u);
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      ah[d] = (pos0 >> 1) == d && (G > 1 || r_l < 8) ? wh : kNone;
+      al[d] = (pos0 >> 1) == d && (G > 1 || r_l < 8) ? wl : kNone;
+    }
+  } else {
+    constexpr int NW = NV / 2;
+#pragma unroll
+    for (int j = 0; j < NW; ++j) {
+      const float p0 = pr[2 * j], p1 = pr[2 * j + 1];
+      const uint32_t wh = kNearest ? pack_bf16x2(p0, p1) : pack_hi16(p0, p1);
+      const float l0 = p0 - bf16_lo(wh), l1 = p1 - bf16_hi(wh);
+      const uint32_t wl = kNearest ? pack_bf16x2(l0, l1) : pack_hi16(l0, l1);
+#pragma unroll
+      for (int d = j; d < 4; d += NW) {          // dword d holds the places 2 d, 2 d + 1
+        ah[d] = r_l == d / NW ? wh : kNone;
+        al[d] = r_l == d / NW ? wl : kNone;
+      }
+    }
+  }
+}
+
+// The accumulators (row r of a channel tile = head r mod G) times c, which lane (l16, q) holds for head l16 mod G.
+template <int G, int NTILE>
+__device__ __forceinline__ void rescale_rows(f32x4_t (&O)[NTILE], float c, int l16, int q) {
+  const float c_other = dpp_f32<0x124>(c);       // G = 8: of the head four further (every lane reads: not inside the choice)
+  const float cq = G < 8 || ((l16 >> 2) & 1) == (q & 1) ? c : c_other;
+  const float ci[4] = {dpp_f32<0x00>(cq), dpp_f32<G == 1 ? 0x00 : 0x55>(cq), dpp_f32<G <= 2 ? 0x00 : 0xAA>(cq),
+                       dpp_f32<G == 1 ? 0x00 : G == 2 ? 0x55 : 0xFF>(cq)};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int nt = 0; nt < NTILE; ++nt) O[nt][i] *= ci[i];
+}
+
+// A wavefront's state into LDS: acc [D][G], ml ([G] maxima, [G] sums).  Rows of the second product: row 4 q + i is head (4 q + i) mod G,
+// lane share (4 q + i) / G.  The shares are added in the lane (G <= 2), then over the lane halves and (G <= 4) the rows of 16 lanes; each
+// exchange pairs two channel tiles, so the lanes end up with different channel tiles and the LDS stores are wide.
+template <int D, int G>
+__device__ __forceinline__ void deposit_state(const f32x4_t (&O)[D / 16], float m_run, float l_tot, float* acc_mine, float* ml_mine, int lane) {
+  constexpr int NTILE = D / 16;
+  const int l16 = lane & 15, q = lane >> 4;
+  constexpr int NH = G < 4 ? G : 4;              // heads per lane
+  float o[NTILE][NH];
+#pragma unroll
+  for (int nt = 0; nt < NTILE; ++nt)
+#pragma unroll
+    for (int h = 0; h < NH; ++h) {
+      if constexpr (G == 1) o[nt][h] = (O[nt][0] + O[nt][1]) + (O[nt][2] + O[nt][3]);
+      else if constexpr (G == 2) o[nt][h] = O[nt][h] + O[nt][h + 2];
+      else o[nt][h] = O[nt][h];
+    }
+#pragma unroll
+  for (int nt = 0; nt < NTILE / 2; ++nt)
+#pragma unroll
+    for (int h = 0; h < NH; ++h) {
+      swap_halves(o[nt][h], o[nt + NTILE / 2][h]);
+      o[nt][h] += o[nt + NTILE / 2][h];
+    }
+  constexpr int NO = G <= 4 ? NTILE / 4 : NTILE / 2;   // channel tiles per lane
+  if constexpr (G <= 4) {
+#pragma unroll
+    for (int nt = 0; nt < NO; ++nt)
+#pragma unroll
+      for (int h = 0; h < NH; ++h) {
+        swap_rows(o[nt][h], o[nt + NO][h]);
+        o[nt][h] += o[nt + NO][h];
+      }
+  }
+  const int nt0 = (NTILE / 2) * (q >> 1) + (G <= 4 ? NO * (q & 1) : 0);
+  const int h0 = G == 8 ? 4 * (q & 1) : 0;
+#pragma unroll
+  for (int nt = 0; nt < NO; ++nt) {
+    float* at = acc_mine + (16 * (nt0 + nt) + l16) * G + h0;
+    if constexpr (NH == 4) *reinterpret_cast<float4*>(at) = make_float4(o[nt][0], o[nt][1], o[nt][2], o[nt][3]);
+    else if constexpr (NH == 2) *reinterpret_cast<float2*>(at) = make_float2(o[nt][0], o[nt][1]);
+    else *at = o[nt][0];
+  }
+  if (q == 0 && l16 < G) {
+    ml_mine[l16] = m_run;
+    ml_mine[G + l16] = l_tot;
+  }
+}
+
 // Everything after the workgroup's kParts partial softmax states (m, l, acc[D] per head) have been
 // deposited in LDS and a barrier has passed: reduce them; a single split finishes the head, otherwise the
 // partial result goes to the workspace and the last workgroup of the head to arrive combines the splits,
