@@ -128,11 +128,16 @@ except ImportError:                      # a torch built without them
 
 # decode_step, decode_step_static, decode_attn and score of the extension; None: through ctypes, 4 us of host time a call more.
 _HOT = ("decode_step", "decode_step_static", "decode_attn", "score")
+_HOT_QUANT = ("decode_step_quant", "decode_attn_quant", "append_quant", "quantize", "dequantize")
 try:
     from . import _pycall
 except ImportError:
     _fast = dict.fromkeys(_HOT)
+    _fast_quant = dict.fromkeys(_HOT_QUANT)
 else:
+    _fast_quant = dict(zip(_HOT_QUANT, _pycall.bind_quant(_raw_stream, _device, C.ArgumentError,
+                                                          *(C.cast(getattr(_lib, "keepkv_" + f), C.c_void_p).value
+                                                            for f in _HOT_QUANT))))
     _fast = dict(zip(_HOT, _pycall.bind(_raw_stream, _device, C.ArgumentError,
                                         *(C.cast(getattr(_lib, "keepkv_" + f), C.c_void_p).value for f in _HOT))))
 
@@ -344,26 +349,40 @@ def select_by_key(layout: Layout, cache: Cache, rank, budget: int, n_sink: int, 
 
 
 def quantize(layout: Layout, src: Cache, dst: QuantCache) -> None:
-    _check(_lib.keepkv_quantize(C.byref(layout.c()), C.byref(src.c()), C.byref(_quant(dst)), _stream()), "keepkv_quantize")
+    fast = _fast_quant["quantize"] if type(layout) is Layout and type(src) is Cache and type(dst) is QuantCache else None
+    _check(fast(layout, src, dst) if fast else
+           _lib.keepkv_quantize(C.byref(layout.c()), C.byref(src.c()), C.byref(_quant(dst)), _stream()), "keepkv_quantize")
 
 
 def dequantize(layout: Layout, src: QuantCache, dst: Cache) -> None:
-    _check(_lib.keepkv_dequantize(C.byref(layout.c()), C.byref(_quant(src)), C.byref(dst.c()), _stream()), "keepkv_dequantize")
+    fast = _fast_quant["dequantize"] if type(layout) is Layout and type(src) is QuantCache and type(dst) is Cache else None
+    _check(fast(layout, src, dst) if fast else
+           _lib.keepkv_dequantize(C.byref(layout.c()), C.byref(_quant(src)), C.byref(dst.c()), _stream()), "keepkv_dequantize")
+
+
+def _fast_quant_call(name: str, layout, cache):
+    return _fast_quant[name] if type(layout) is Layout and type(cache) is QuantCache else None
 
 
 def append_quant(layout: Layout, cache: QuantCache, k_t, v_t, n_tokens: int = 1, counts=None, overflow=None) -> None:
-    _check(_lib.keepkv_append_quant(C.byref(layout.c()), C.byref(_quant(cache)), _ptr(k_t), _ptr(v_t), n_tokens, _ptr(counts),
+    fast = _fast_quant_call("append_quant", layout, cache)
+    _check(fast(layout, cache, k_t, v_t, n_tokens, counts, overflow) if fast else
+           _lib.keepkv_append_quant(C.byref(layout.c()), C.byref(_quant(cache)), _ptr(k_t), _ptr(v_t), n_tokens, _ptr(counts),
                                     _ptr(overflow), _stream()), "keepkv_append_quant")
 
 
 def decode_attn_quant(layout: Layout, cache: QuantCache, q, out, logits_out, lse_out, workspace) -> None:
-    _check(_lib.keepkv_decode_attn_quant(C.byref(layout.c()), C.byref(_quant(cache)), _ptr(q), _ptr(out), _ptr(logits_out),
+    fast = _fast_quant_call("decode_attn_quant", layout, cache)
+    _check(fast(layout, cache, q, out, logits_out, lse_out, workspace) if fast else
+           _lib.keepkv_decode_attn_quant(C.byref(layout.c()), C.byref(_quant(cache)), _ptr(q), _ptr(out), _ptr(logits_out),
                                          _ptr(lse_out), _ptr(workspace), _nbytes(workspace), _stream()),
            "keepkv_decode_attn_quant")
 
 
 def decode_step_quant(layout: Layout, cache: QuantCache, q, k_t, v_t, out, logits_out, alpha: float, overflow, workspace) -> None:
-    _check(_lib.keepkv_decode_step_quant(C.byref(layout.c()), C.byref(_quant(cache)), _ptr(q), _ptr(k_t), _ptr(v_t), _ptr(out),
+    fast = _fast_quant_call("decode_step_quant", layout, cache)
+    _check(fast(layout, cache, q, k_t, v_t, out, logits_out, alpha, overflow, workspace) if fast else
+           _lib.keepkv_decode_step_quant(C.byref(layout.c()), C.byref(_quant(cache)), _ptr(q), _ptr(k_t), _ptr(v_t), _ptr(out),
                                          _ptr(logits_out), alpha, _ptr(overflow), _ptr(workspace), _nbytes(workspace),
                                          _stream()), "keepkv_decode_step_quant")
 

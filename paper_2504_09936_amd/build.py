@@ -12,7 +12,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkeepkv.so")
 PYCALL = os.path.join(HERE, "_pycall.so")
-SOURCES = ["api.hip", "decode_attn.hip", "decode_quant.hip", "quant_cache.hip", "score_append.hip", "score_window.hip", "select.hip", "match.hip", "merge.hip", "probe.hip"]
+SOURCES = ["api.hip", "decode_attn.hip", "decode_quant.hip", "decode_quant_bf16_64.hip", "decode_quant_bf16_128.hip",
+           "decode_quant_f32_64.hip", "decode_quant_f32_128.hip", "quant_cache.hip", "score_append.hip", "score_window.hip", "select.hip", "match.hip", "merge.hip", "probe.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-mllvm", "-amdgpu-mfma-vgpr-form",   # MFMA results in VGPRs: the fused epilogue reads them directly

@@ -1170,21 +1170,6 @@ static void choose_split_valu(const keepkv_layout* L, int capacity, long& per) {
   }
 }
 
-static size_t decode_bytes(const keepkv_layout* L, long nsplit) {
-  return kWorkspaceHead + align_up((size_t)L->batch * L->n_q_heads * nsplit * (L->head_dim + 2) * sizeof(float), 256);
-}
-
-// Partial results with cache lines of their own, for heads that are combined within an XCD.
-static size_t decode_xcd_bytes(const keepkv_layout* L, long nsplit) {
-  return kWorkspaceHead + kLine + align_up((size_t)L->batch * L->n_kv_heads * nsplit * xcd_split_stride(L) * sizeof(float), 256);
-}
-
-// The heads have to divide evenly among the XCDs, or some would idle; with 4 heads, say, half of them.
-static bool heads_fit_xcds(const keepkv_layout* L) {
-  const long units = (long)L->batch * L->n_kv_heads;
-  return units % 8 == 0 && units <= kMaxXcdUnits;
-}
-
 // Where combining within an XCD pays.  Measured through memory / within the XCD, us: with one tile a wavefront always, or it makes no
 // difference (250 shapes, 4 % on average): 8 heads x 852 slots in seven splits 6.5 / 6.2, 64 x 852 in four 10.0 / 9.6, 32 x 1497 in eight 9.9 / 9.4.
 // With two tiles the tail is a smaller share of the step, and how soon a head's workgroups have all arrived matters more.  D 128: 64 x 1487
@@ -1238,24 +1223,8 @@ size_t decode_workspace_bytes(const keepkv_layout* L, int capacity) {
   return bytes;
 }
 
-// The cost model walks up to 1024 candidate plans, microseconds of host time, and a program asks for the same
-// few plans again and again (one per layer shape and step): each thread keeps its last ones.  A plan is a pure function
-// of the fields compared here.
 static DecodePlan kept_plan(const keepkv_layout* L, int capacity, int force_per, int force_waves, bool charge) {
-  struct Entry {
-    int32_t key[9];
-    DecodePlan plan;
-  };
-  static thread_local Entry kept[8] = {};          // (a zero batch is no valid key)
-  const int32_t key[9] = {L->batch, L->n_q_heads, L->n_kv_heads, L->head_dim, L->dtype, capacity, force_per, force_waves, charge};
-  uint32_t h = 0;
-  for (int32_t k : key) h = h * 31u + (uint32_t)k;
-  Entry& e = kept[(h ^ (h >> 15)) & 7u];
-  if (memcmp(e.key, key, sizeof key) != 0) {
-    e.plan = make_plan(L, capacity, force_per, force_waves, charge);
-    memcpy(e.key, key, sizeof key);
-  }
-  return e.plan;
+  return kept_plan_of(L, capacity, force_per, force_waves, charge, make_plan);
 }
 DecodePlan plan_decode(const keepkv_layout* L, int capacity, int force_per, int force_waves) {
   return kept_plan(L, capacity, force_per, force_waves, true);

@@ -4,6 +4,7 @@
 #pragma once
 
 #include <math.h>
+#include <string.h>
 
 #include <type_traits>
 #include <utility>
@@ -20,8 +21,6 @@ static __device__ long long kk_trace[8 * 8192];
 #else
 #define KK_TS(i) do { } while (0)
 #endif
-
-namespace {
 
 struct DecodeParams {
   const void* q;
@@ -52,6 +51,8 @@ struct DecodeParams {
   float scale;
   float ln_alpha, ln_1m_alpha;
 };
+
+namespace {
 
 // Control words of heads whose workgroups may share an XCD: at most kMaxXcdUnits heads, behind their tickets.
 constexpr int kMaxXcdUnits = 2048;
@@ -556,6 +557,43 @@ __device__ __forceinline__ void combine_and_finish(const DecodeParams& p, const 
     if (STEP && grow) p.len[unit] = len;
     if (STEP && !grow && p.overflow != nullptr) *p.overflow = 1;
   }
+}
+
+// ---- plans (host) ----------------------------------------------------------------------------------------------
+inline size_t decode_bytes(const keepkv_layout* L, long nsplit) {
+  return kWorkspaceHead + align_up((size_t)L->batch * L->n_q_heads * nsplit * (L->head_dim + 2) * sizeof(float), 256);
+}
+
+// Partial results with cache lines of their own, for heads that are combined within an XCD.
+inline size_t decode_xcd_bytes(const keepkv_layout* L, long nsplit) {
+  return kWorkspaceHead + kLine + align_up((size_t)L->batch * L->n_kv_heads * nsplit * xcd_split_stride(L) * sizeof(float), 256);
+}
+
+// The heads have to divide evenly among the XCDs, or some would idle; with 4 heads, say, half of them.
+inline bool heads_fit_xcds(const keepkv_layout* L) {
+  const long units = (long)L->batch * L->n_kv_heads;
+  return units % 8 == 0 && units <= kMaxXcdUnits;
+}
+
+// The cost model walks up to 1024 candidate plans, microseconds of host time, and a program asks for the same
+// few plans again and again (one per layer shape and step): each thread keeps its last ones.  A plan is a pure function
+// of the fields compared here.
+template <typename Make>
+inline DecodePlan kept_plan_of(const keepkv_layout* L, int capacity, int force_per, int force_waves, bool charge, Make make) {
+  struct Entry {
+    int32_t key[9];
+    DecodePlan plan;
+  };
+  static thread_local Entry kept[8] = {};          // (a zero batch is no valid key)
+  const int32_t key[9] = {L->batch, L->n_q_heads, L->n_kv_heads, L->head_dim, L->dtype, capacity, force_per, force_waves, charge};
+  uint32_t h = 0;
+  for (int32_t k : key) h = h * 31u + (uint32_t)k;
+  Entry& e = kept[(h ^ (h >> 15)) & 7u];
+  if (memcmp(e.key, key, sizeof key) != 0) {
+    e.plan = make(L, capacity, force_per, force_waves, charge);
+    memcpy(e.key, key, sizeof key);
+  }
+  return e.plan;
 }
 
 }  // namespace

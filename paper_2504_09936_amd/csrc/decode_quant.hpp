@@ -1,0 +1,502 @@
+// The kernel of keepkv_decode_attn_quant / keepkv_decode_step_quant: Eq. 6 over a cache of e4m3 codes, optionally with the append of a
+// token (quantised as keepkv_append_quant does it) and the EMA score update (Eq. 8).  Sources of their own instantiate launch_quant
+// for a dtype and head dimension each, so that they compile side by side.
+#pragma once
+
+#include <type_traits>
+#include <utility>
+
+#include "decode_common.hpp"
+#include "quant_launch.hpp"
+
+namespace kk {
+namespace {
+
+// A wavefront owns tiles of 32 slots, which are the blocks that share a scale, and takes both products to the matrix cores (16x16x32,
+// bf16 operands): a code times its scale has 4 significant bits, so it is exact in bf16, and the conversion instruction applies the scale.
+// The query stays as it is (f32 queries as three bf16 terms, 24 bits) and products are summed in f32.
+//
+// K rows travel straight into registers in the layout of the A operand: the sum over channels may run in any order, so lane (row l16,
+// quarter q) takes the 16 bytes at 64 h + 16 q (h = 0, 1) and the queries are read in that order.  V rows go to LDS by asynchronous
+// copies, and ds_read_b64_tr_b8 returns a channel's 8 slots of a lane in the order in which the scores lie (checked on
+// the device).  16-byte chunk c of row r sits at position c ^ swizzle(r), so that the 8 rows of a transposed read lie in different banks.
+//
+// The appended token is a row of the block that its slot lies in, so the wavefront of that tile quantises it, moves the block's codes to a
+// larger scale if the token needs one (in registers and LDS, and back to memory), and puts the row in before the products.  No other wavefront
+// reads that block.
+template <int D>
+__device__ __forceinline__ int swizzle(int row) {
+  if constexpr (D == 128) return (row & 3) | ((row >> 4) & 1) << 2;   // rows of 128 bytes: 4 q + i and 16 + 4 q + i apart
+  else return ((row >> 1) & 1) | ((row >> 4) & 1) << 1;               // two rows to 128 bytes
+}
+
+// 8 codes (two words) times the scale, in bf16: exact
+__device__ __forceinline__ bf16x8_t expand8(uint32_t lo, uint32_t hi, float scale) {
+  const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+  const bf16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+  return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+__device__ __forceinline__ float uniform_f32(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+}
+
+// LDS of a wavefront: kBuffers V tiles, later its deposit (and the weights of the splits behind it).
+constexpr int quant_wave_bytes(int D, int G, int buffers) {
+  const int tiles = buffers * kQBlock * D, deposit = (G * D + 16 + 128) * 4;
+  return (tiles > deposit ? tiles : deposit + 127) / 128 * 128;
+}
+constexpr int kStageSlots = 256;                 // of a wavefront: new scores that wait in LDS for the end of a tile loop
+
+// How many tiles a wavefront has at most: one, two (all requested before the first wait), more (a loop over two buffers); and where splits
+// meet: not at all, through memory, or within an XCD where their workgroups find that they may.
+constexpr int kOne = 0, kTwo = 1, kLoop = 2;
+constexpr int kSoloMeet = 0, kMemMeet = 1, kXcdMeet = 2;
+
+template <typename T, int D, int G, bool STEP, int kTiles, int kMeet, int kWaves>
+__global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantParams qp) {
+  const DecodeParams& p = qp.d;
+  constexpr bool kF32 = sizeof(T) == 4;
+  constexpr int KH = D / 64, KS = D / 32, NTILE = D / 16, CHUNKS = D / 16;
+  constexpr int TILE_BYTES = kQBlock * D, VLOADS = TILE_BYTES / (kWave * 16);
+  constexpr int NV = kShare<G>;
+  constexpr int kBuffers = kTiles == kOne ? 1 : 2;
+  constexpr int WAVE_BYTES = quant_wave_bytes(D, G, kBuffers);
+  constexpr int QTERMS = kF32 ? 3 : 1;
+  constexpr int REQUESTS = 2 * KH + 2 + (STEP ? 1 : 0) + VLOADS;      // of a tile
+  constexpr int EPL = D / kWave;                 // channels of a lane in an appended row
+  extern __shared__ __align__(256) unsigned char smem_tiles[];
+  constexpr bool kMayShareXcd = kMeet == kXcdMeet;
+  __shared__ int s_last, s_one_xcd;
+  __shared__ __align__(16) unsigned char s_new[2 * D];                // the appended token's codes: K, V
+
+  const int unit = kMayShareXcd ? (int)(blockIdx.z * 8 + blockIdx.x) : (int)blockIdx.y;
+  const int split = kMayShareXcd ? blockIdx.y : blockIdx.x;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, q = lane >> 4;
+  const int len_old = p.len[unit];
+  const int t_old = STEP ? p.t_obs[unit] : 0;
+  const int start = split * p.per;
+  const size_t ubase = (size_t)unit * p.capacity;
+  const int blocks = quant_blocks(p.capacity);
+  const uint8_t* kbytes = reinterpret_cast<const uint8_t*>(p.k) + ubase * D;
+  const uint8_t* vbytes = reinterpret_cast<const uint8_t*>(p.v) + ubase * D;
+  const float* scales = (lane & 1 ? qp.v_scale : qp.k_scale) + (size_t)unit * blocks;
+  unsigned char* const Tb = smem_tiles + wave * WAVE_BYTES;
+
+  // slots that may be read (len itself, or the caller's bound on it, so that nothing waits for len); tiles up to `lim`
+  const int bound = p.len_hint > 0 ? min(p.len_hint, p.capacity) : len_old;
+  const int lim = min(min(bound + (STEP ? 1 : 0), p.capacity), start + p.per);
+  const int last_row = max(bound - 1, 0);
+
+  const int g_l = l16 % G, r_l = l16 / G;
+  const int pos0 = (r_l * NV) & 7;
+  const int row0 = 16 * (pos0 >> 2) + 4 * q + (pos0 & 3);
+  const int row_mine = row0 + (g_l & (NV - 1));
+  const bool writer = G == 1 ? r_l < 8 : g_l < NV;
+
+  // This workgroup has arrived (the last wavefront, whose share is the shortest), ahead of its requests.
+  if (kMayShareXcd && wave == kWaves - 1 && lane == 0)
+    __hip_atomic_fetch_add(&p.arrivals[unit], 1ull << (8 * xcd_id()), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+
+  // ---- requests
+  bf16x8_t qb[QTERMS][KS];                       // column l16 is head l16 mod G, this lane's channels 64 h + 16 q + 8 t + j of k-step 2 h + t
+  {
+    const T* qrow = reinterpret_cast<const T*>(p.q) + ((size_t)unit * G + g_l) * D + 16 * q;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const T* at = qrow + 64 * (ks >> 1) + 8 * (ks & 1);
+      if constexpr (!kF32) {
+        qb[0][ks] = *reinterpret_cast<const bf16x8_t*>(at);
+      } else {
+        const float4 a = *reinterpret_cast<const float4*>(at), b = *reinterpret_cast<const float4*>(at + 4);
+        float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int t = 0; t < 3; ++t) {            // each term takes the 8 leading bits of what is left
+          uint32_t w[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] = pack_hi16(x[2 * i], x[2 * i + 1]);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] -= __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x[i]) & 0xFFFF0000u);
+          qb[t][ks] = __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
+        }
+      }
+    }
+  }
+  float k_new[EPL], v_new[EPL];                  // STEP: this lane's channels EPL lane .. of the token
+  if constexpr (STEP) {
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) {
+      const size_t at = (size_t)unit * D + lane * EPL + e;
+      k_new[e] = kF32 ? reinterpret_cast<const float*>(p.k_t)[at] : bf16_to_f32(reinterpret_cast<const uint16_t*>(p.k_t)[at]);
+      v_new[e] = kF32 ? reinterpret_cast<const float*>(p.v_t)[at] : bf16_to_f32(reinterpret_cast<const uint16_t*>(p.v_t)[at]);
+    }
+  }
+  struct Tile {
+    u32x4_t k[2][KH];
+    float scale;                                 // of K in even lanes, of V in odd ones
+    int votes;
+    float ls;                                    // ln S of slot row_mine
+  };
+  auto request = [&](int tbase, Tile& t, unsigned char* buf) {
+    t.scale = scales[min(tbase / kQBlock, blocks - 1)];
+    const int at = min(tbase + row_mine, last_row);
+    t.votes = p.votes[ubase + at];
+    if constexpr (STEP) t.ls = p.log_s[ubase + at];
+    else t.ls = 0.f;
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+      const uint32_t off = (uint32_t)(min(tbase + 16 * st + l16, last_row) * D + 16 * q);
+#pragma unroll
+      for (int h = 0; h < KH; ++h) t.k[st][h] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(kbytes + off + 64 * h));
+    }
+#pragma unroll
+    for (int i = 0; i < VLOADS; ++i) {
+      const int at16 = i * kWave + lane, row = at16 / CHUNKS, chunk = (at16 % CHUNKS) ^ swizzle<D>(row);
+      copy_to_lds<2>(vbytes, (size_t)(last_row + 1) * D, buf + i * (kWave * 16), (uint32_t)(min(tbase + row, last_row) * D + 16 * chunk), 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  const bool grow = STEP && len_old < p.capacity;
+  const int len = grow ? len_old + 1 : len_old;
+  const int live_end = min(len, start + p.per);
+  const int new_row = len_old % kQBlock;
+  const int own_base = grow ? len_old - new_row : -1;                 // the tile that the appended token joins
+
+  const float sl2 = p.scale * kLog2e;
+  float m_run = kLowest, l_run = 0.f;
+  f32x4_t O[NTILE];
+#pragma unroll
+  for (int nt = 0; nt < NTILE; ++nt) O[nt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+  auto scale_for = [&](const float (&x)[EPL], float old, uint32_t& bits) {   // of the block with the new row
+    float a = 0.f;
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) a = fmaxf(a, __builtin_bit_cast(float, finite_magnitude(x[e])));
+    a = over_head_lanes<1>(a, [](float u, float v) { return fmaxf(u, v); });
+    bits = scale_bits(__builtin_bit_cast(uint32_t, a));
+    const uint32_t had = __builtin_bit_cast(uint32_t, old);
+    if (new_row > 0) bits = max(bits, had);
+    bits = __builtin_amdgcn_readfirstlane(bits);
+    return new_row > 0 && bits != had;           // the live codes move to the larger scale
+  };
+  auto encode_row = [&](const float (&x)[EPL], uint32_t bits, unsigned char* at) {
+    const float inv = inverse_scale(bits);
+    if constexpr (EPL == 2) *reinterpret_cast<uint16_t*>(at + 2 * lane) = (uint16_t)encode4(x[0] * inv, x[1] * inv, 0.f, 0.f);
+    else at[lane] = (unsigned char)encode4(x[0] * inv, 0.f, 0.f, 0.f);
+  };
+  bool wrote = false;                            // (uniform) this wavefront has the appended row
+  uint32_t new_ks = 0, new_vs = 0;
+
+  // The first wavefront requests the head's `arrivals` when its last tile's rows have landed, to have the word when the tile is done.
+  uint64_t seen = 0;
+  bool looked = !kMayShareXcd || wave != 0;      // uniform
+  auto look = [&]() {
+    if (!looked) seen = ld_arrivals(p, unit);
+    looked = true;
+  };
+
+  // One tile; V has landed when at most v_wait requests are outstanding.  Returns the group-mean logit of slot row_mine and whether this lane
+  // stores it.
+  // first: no tile of this wavefront has been computed.
+  auto compute = [&](int tbase, Tile& t, unsigned char* Vb, bool first, auto v_wait, float& x_out, float& ls_old) -> bool {
+    constexpr int kVWait = decltype(v_wait)::value;
+    const int n_live = min(kQBlock, live_end - tbase);
+    x_out = ls_old = 0.f;
+    if (n_live <= 0) return false;               // uniform: below the caller's bound but dead, its scales mean nothing
+    float ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, t.scale), 0));
+    float vs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, t.scale), 1));
+    const bool own = STEP && tbase == own_base;  // uniform
+    bool v_moves = false;
+    float v_ratio = 1.f;
+    if (own) {
+      wrote = true;
+      const bool k_moves = scale_for(k_new, ks, new_ks);
+      if (k_moves) {
+        const float ratio = ks * inverse_scale(new_ks);
+#pragma unroll
+        for (int st = 0; st < 2; ++st)
+#pragma unroll
+          for (int h = 0; h < KH; ++h) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t.k[st][h][i] = shift_codes(t.k[st][h][i], ratio);
+            const int r = 16 * st + l16;
+            if (r < new_row) *reinterpret_cast<u32x4_t*>(const_cast<uint8_t*>(kbytes) + (size_t)(tbase + r) * D + 64 * h + 16 * q) = t.k[st][h];
+          }
+      }
+      ks = __builtin_bit_cast(float, new_ks);
+      v_moves = scale_for(v_new, vs, new_vs);
+      v_ratio = vs * inverse_scale(new_vs);
+      vs = __builtin_bit_cast(float, new_vs);
+      encode_row(k_new, new_ks, s_new);
+      encode_row(v_new, new_vs, s_new + D);
+      __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int h = 0; h < KH; ++h) {
+        const u32x4_t w = *reinterpret_cast<const u32x4_t*>(s_new + 64 * h + 16 * q);
+#pragma unroll
+        for (int st = 0; st < 2; ++st) t.k[st][h] = 16 * st + l16 == new_row ? w : t.k[st][h];
+      }
+    }
+    // ---- S^T = K Q^T
+    f32x4_t s[2] = {f32x4_t{0.f, 0.f, 0.f, 0.f}, f32x4_t{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int term = QTERMS - 1; term >= 0; --term)
+#pragma unroll
+      for (int k_step = 0; k_step < KS; ++k_step)
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+          const u32x4_t w = t.k[st][k_step >> 1];
+          s[st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(expand8(w[2 * (k_step & 1)], w[2 * (k_step & 1) + 1], ks), qb[term][k_step], s[st], 0, 0, 0);
+        }
+    float sv[NV];
+    take_shares<G>(s, r_l, pos0, sv);
+    // ---- logits (log2 domain, log2(votes) folded in), group-mean logit for the EMA
+    const bool mine_new = own && row_mine == new_row;
+    const float lp_lane = mine_new ? 0.f : fast_log2((float)t.votes);
+    ls_old = mine_new ? -INFINITY : t.ls;
+    float z[NV], xm[NV], lp[NV];
+    if constexpr (NV == 1) lp[0] = lp_lane;
+    else {                                       // slot row0 + v is loaded by lane v of the quad
+      lp[0] = dpp_f32<0x00>(lp_lane);
+      lp[1] = dpp_f32<0x55>(lp_lane);
+      if constexpr (NV == 4) {
+        lp[2] = dpp_f32<0xAA>(lp_lane);
+        lp[3] = dpp_f32<0xFF>(lp_lane);
+      }
+    }
+    float tm = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const bool live = row0 + v < n_live && (G > 1 || r_l < 8);
+      z[v] = live ? fmaf(sv[v], sl2, lp[v]) : -INFINITY;
+      tm = fmaxf(tm, z[v]);
+      xm[v] = head_sum<G>(sv[v]);
+    }
+    const float mn = fmaxf(m_run, over_head_lanes<G>(tm, [](float a, float b) { return fmaxf(a, b); }));
+    const float c = fast_exp2(m_run - mn);
+    float pr[NV], ps = 0.f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      pr[v] = fast_exp2(z[v] - mn);
+      ps += pr[v];
+    }
+    l_run = fmaf(l_run, c, ps);
+    m_run = mn;
+    if (!first && __any(c != 1.f)) rescale_rows<G>(O, c, l16, q);
+    // (tied to the softmax sum, so that the wait is not scheduled ahead of the arithmetic it is meant to hide)
+    asm volatile("s_waitcnt vmcnt(%1)" : "+v"(l_run) : "n"(kVWait) : "memory");
+    if (kVWait == 0) look();
+    if (n_live < kQBlock || own) {               // uniform
+      if (v_moves) {
+        for (int i = lane; i < new_row * CHUNKS; i += kWave) {
+          uint4* at = reinterpret_cast<uint4*>(Vb) + i;
+          uint4 w = *at;
+          w = make_uint4(shift_codes(w.x, v_ratio), shift_codes(w.y, v_ratio), shift_codes(w.z, v_ratio), shift_codes(w.w, v_ratio));
+          *at = w;
+          const int row = i / CHUNKS, chunk = (i % CHUNKS) ^ swizzle<D>(row);
+          *reinterpret_cast<uint4*>(const_cast<uint8_t*>(vbytes) + (size_t)(tbase + row) * D + 16 * chunk) = w;
+        }
+      }
+      // rows of masked slots are cleared (0 * NaN would be NaN)
+      for (int i = n_live * CHUNKS + lane; i < kQBlock * CHUNKS; i += kWave) reinterpret_cast<uint4*>(Vb)[i] = make_uint4(0, 0, 0, 0);
+      if (own && lane < CHUNKS)
+        reinterpret_cast<uint4*>(Vb)[new_row * CHUNKS + (lane ^ swizzle<D>(new_row))] = *reinterpret_cast<const uint4*>(s_new + D + 16 * lane);
+      __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+    // ---- O += P V
+    uint32_t aw[2][4];
+    weights_operand<G, true>(pr, r_l, pos0, aw[0], aw[1]);
+    const int vrow = 16 * (l16 >> 3) + 4 * q + ((l16 >> 1) & 3);      // the row whose half this lane's address names
+    typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
+    u32x2_t b[NTILE];
+    uint32_t va[NTILE];
+    const uint32_t va0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)Vb +
+                         (uint32_t)(vrow * D + swizzle<D>(vrow) * 16 + (l16 & 1) * 8);
+#pragma unroll
+    for (int nt = 0; nt < NTILE; ++nt) va[nt] = va0 ^ (uint32_t)(nt * 16);
+    if constexpr (NTILE == 8)
+      asm volatile(
+          "ds_read_b64_tr_b8 %0, %8\n\tds_read_b64_tr_b8 %1, %9\n\tds_read_b64_tr_b8 %2, %10\n\tds_read_b64_tr_b8 %3, %11\n\t"
+          "ds_read_b64_tr_b8 %4, %12\n\tds_read_b64_tr_b8 %5, %13\n\tds_read_b64_tr_b8 %6, %14\n\tds_read_b64_tr_b8 %7, %15\n\t"
+          "s_waitcnt lgkmcnt(0)"
+          : "=&v"(b[0]), "=&v"(b[1]), "=&v"(b[2]), "=&v"(b[3]), "=&v"(b[4]), "=&v"(b[5]), "=&v"(b[6]), "=&v"(b[7])
+          : "v"(va[0]), "v"(va[1]), "v"(va[2]), "v"(va[3]), "v"(va[4]), "v"(va[5]), "v"(va[6]), "v"(va[7])
+          : "memory");
+    else
+      asm volatile(
+          "ds_read_b64_tr_b8 %0, %4\n\tds_read_b64_tr_b8 %1, %5\n\tds_read_b64_tr_b8 %2, %6\n\tds_read_b64_tr_b8 %3, %7\n\t"
+          "s_waitcnt lgkmcnt(0)"
+          : "=&v"(b[0]), "=&v"(b[1]), "=&v"(b[2]), "=&v"(b[3])
+          : "v"(va[0]), "v"(va[1]), "v"(va[2]), "v"(va[3])
+          : "memory");
+#pragma unroll
+    for (int part = 0; part < 2; ++part)
+#pragma unroll
+      for (int nt = 0; nt < NTILE; ++nt)
+        O[nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, make_uint4(aw[part][0], aw[part][1], aw[part][2], aw[part][3])),
+                                                        expand8(b[nt][0], b[nt][1], vs), O[nt], 0, 0, 0);
+    float x = xm[0];
+#pragma unroll
+    for (int v = 1; v < NV; ++v) x = (g_l & (NV - 1)) == v ? xm[v] : x;
+    x_out = x * (p.scale * (1.0f / G));
+    return writer && row_mine < n_live;
+  };
+  auto ema = [&](float ls_old, float x) {        // ln(alpha S + (1 - alpha) e^x)
+    const float a = p.ln_alpha + ls_old, b = p.ln_1m_alpha + x;
+    const float hi = fmaxf(a, b), lo = fminf(a, b);
+    return (lo == -INFINITY) ? hi : hi + kLn2 * fast_log2(1.f + fast_exp2((lo - hi) * kLog2e));
+  };
+
+  unsigned char* const s_stage = smem_tiles + kWaves * WAVE_BYTES;
+  const bool staged = kTiles == kLoop && STEP && p.per <= kWaves * kStageSlots;
+  constexpr int kTileStep = kWaves * kQBlock;
+  constexpr std::integral_constant<int, 0> kAll{};
+  constexpr std::integral_constant<int, REQUESTS> kFirst{};
+  const int base = start + wave * kQBlock;
+  bool own0 = false, own1 = false;               // results per slot that are stored at the very end
+  float x0 = 0.f, x1 = 0.f, ls0 = 0.f, ls1 = 0.f;
+  Tile t0, t1;
+  if constexpr (kTiles == kOne) {
+    if (base < lim) {
+      request(base, t0, Tb);
+      own0 = compute(base, t0, Tb, true, kAll, x0, ls0);
+    }
+  } else if constexpr (kTiles == kTwo) {
+    if (base < lim) {
+      request(base, t0, Tb);
+      request(base + kTileStep, t1, Tb + TILE_BYTES);                 // (beyond the last row its rows are the last row's)
+      own0 = compute(base, t0, Tb, true, kFirst, x0, ls0);
+      if (base + kTileStep < lim) own1 = compute(base + kTileStep, t1, Tb + TILE_BYTES, false, kAll, x1, ls1);
+    }
+  } else {
+    auto publish = [&](int tbase, bool mine, float x, float ls_old) {
+      if (p.logits_out != nullptr && mine) p.logits_out[ubase + tbase + row_mine] = x;
+      if constexpr (STEP) {
+        const float r = ema(ls_old, x);
+        if (mine) {
+          if (staged) {
+            const uint32_t sa = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)(s_stage + (size_t)(tbase - start + row_mine) * 4);
+            asm volatile("ds_write_b32 %0, %1" : : "v"(sa), "v"(r) : "memory");
+          } else {
+            p.log_s[ubase + tbase + row_mine] = r;
+          }
+        }
+      }
+    };
+    // two tiles in flight: a tile's buffer is requested again when it has been used (beyond the last row: the last row again)
+    if (base < lim) {
+      request(base, t0, Tb);
+      request(base + kTileStep, t1, Tb + TILE_BYTES);
+    }
+    for (int tb = base; tb < lim; tb += 2 * kTileStep) {
+      float x, ls;
+      bool mine = compute(tb, t0, Tb, tb == base, kFirst, x, ls);
+      publish(tb, mine, x, ls);
+      __builtin_amdgcn_sched_barrier(0);
+      request(tb + 2 * kTileStep, t0, Tb);
+      if (tb + kTileStep < lim) {
+        mine = compute(tb + kTileStep, t1, Tb + TILE_BYTES, false, kFirst, x, ls);
+        publish(tb + kTileStep, mine, x, ls);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      request(tb + 3 * kTileStep, t1, Tb + TILE_BYTES);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                  // no copy may land in what follows
+  }
+
+  // ---- this wavefront's state, then the workgroup's
+  const float l_tot = over_head_lanes<G>(l_run, [](float a, float b) { return a + b; });
+  constexpr int kPartStride = WAVE_BYTES / 4;
+  float* s_acc = reinterpret_cast<float*>(smem_tiles);
+  float* s_ml = s_acc + G * D;
+  if constexpr (kTiles != kLoop) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (the copies of a tile that was passed over)
+  deposit_state<D, G>(O, m_run, l_tot, s_acc + wave * kPartStride, s_ml + wave * kPartStride, lane);
+  if (threadIdx.x == 0) {
+    look();                                      // (a wavefront without a tile)
+    s_one_xcd = kMayShareXcd && all_on_this_xcd(p, unit, seen);
+  }
+  if constexpr (kTiles == kLoop && STEP) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the staged scores are in LDS
+  __syncthreads();
+  if constexpr (kTiles != kLoop) {
+    auto store = [&](int tbase, bool mine, float x, float ls_old) {
+      const size_t at = ubase + tbase + row_mine;
+      if (p.logits_out != nullptr && mine) p.logits_out[at] = x;
+      if (STEP && mine) p.log_s[at] = ema(ls_old, x);
+    };
+    store(base, own0, x0, ls0);
+    if constexpr (kTiles == kTwo) store(base + kTileStep, own1, x1, ls1);
+  } else if constexpr (STEP) {
+    if (staged)
+      for (int j = threadIdx.x; j < live_end - start; j += kWaves * kWave)
+        __hip_atomic_store(&p.log_s[ubase + start + j], *reinterpret_cast<const float*>(s_stage + (size_t)j * 4), __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
+  }
+  if (STEP && wrote) {                           // the appended token joins the cache
+    if (lane < 2 * CHUNKS) {
+      uint8_t* dst = const_cast<uint8_t*>(lane < CHUNKS ? kbytes : vbytes) + (size_t)len_old * D;
+      reinterpret_cast<uint4*>(dst)[lane % CHUNKS] = *reinterpret_cast<const uint4*>(s_new + lane * 16);
+    }
+    if (lane == 0) {
+      p.votes[ubase + len_old] = 1;
+      p.born[ubase + len_old] = t_old;
+      qp.k_scale[(size_t)unit * blocks + len_old / kQBlock] = __builtin_bit_cast(float, new_ks);
+      qp.v_scale[(size_t)unit * blocks + len_old / kQBlock] = __builtin_bit_cast(float, new_vs);
+    }
+  }
+  combine_and_finish<T, D, G, kWaves, STEP, kWaves, true, kMeet == kSoloMeet, kMayShareXcd>(p, s_ml, s_ml + G, s_acc, kPartStride, kPartStride, &s_last,
+                                                                                             unit, split, grow, len, t_old,
+                                                                                             __builtin_amdgcn_readfirstlane(s_one_xcd) != 0);
+}
+
+template <typename T, int D, int G>
+keepkv_status launch_quant_g(const QuantParams& p, int units, bool step, hipStream_t st) {
+  auto go = [&](auto step_tag, auto tiles_tag, auto meet_tag, auto waves_tag) -> keepkv_status {
+    constexpr int kTiles = decltype(tiles_tag)::value, kWaves = decltype(waves_tag)::value;
+    constexpr size_t lds = (size_t)kWaves * (quant_wave_bytes(D, G, kTiles == kOne ? 1 : 2) + (kTiles == kLoop ? kStageSlots * 4 : 0));
+    auto* kernel = decode_quant_kernel<T, D, G, decltype(step_tag)::value, kTiles, decltype(meet_tag)::value, kWaves>;
+    if constexpr (lds > 60 * 1024) {
+      static const bool allowed = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) == hipSuccess;
+      if (!allowed) return KEEPKV_ERR_DEVICE;
+    }
+    // (x, then y, is dealt first: with 8 heads along x the splits of a head come to one XCD, see all_on_this_xcd)
+    const dim3 grid = decltype(meet_tag)::value == kXcdMeet ? dim3(8, p.d.nsplit, units / 8) : dim3(p.d.nsplit, units);
+    kernel<<<grid, kWaves * kWave, lds, st>>>(p);
+    return launch_status();
+  };
+  auto by_waves = [&](auto step_tag, auto tiles_tag, auto meet_tag) {
+    if (p.d.waves == 8) return go(step_tag, tiles_tag, meet_tag, std::integral_constant<int, 8>{});
+    return go(step_tag, tiles_tag, meet_tag, std::integral_constant<int, 4>{});
+  };
+  auto by_meet = [&](auto step_tag, auto tiles_tag) {
+    if (p.d.nsplit == 1) return by_waves(step_tag, tiles_tag, std::integral_constant<int, kSoloMeet>{});
+    if constexpr (sizeof(T) == 2 && decltype(tiles_tag)::value != kLoop)
+      if (p.d.arrivals != nullptr) return by_waves(step_tag, tiles_tag, std::integral_constant<int, kXcdMeet>{});
+    return by_waves(step_tag, tiles_tag, std::integral_constant<int, kMemMeet>{});
+  };
+  const int n_tiles = (p.d.per + p.d.waves * kQBlock - 1) / (p.d.waves * kQBlock);      // of a wavefront, at most
+  auto by_tiles = [&](auto step_tag) {
+    if (n_tiles == 1) return by_meet(step_tag, std::integral_constant<int, kOne>{});
+    if constexpr (sizeof(T) == 2)                // (f32 layouts, which no large cache has, do with the loop)
+      if (n_tiles == 2) return by_meet(step_tag, std::integral_constant<int, kTwo>{});
+    return by_meet(step_tag, std::integral_constant<int, kLoop>{});
+  };
+  return step ? by_tiles(std::true_type{}) : by_tiles(std::false_type{});
+}
+
+}  // namespace
+
+template <typename T, int D>
+keepkv_status launch_quant(const QuantParams& p, int units, int G, bool step, hipStream_t st) {
+  switch (G) {
+    case 1: return launch_quant_g<T, D, 1>(p, units, step, st);
+    case 2: return launch_quant_g<T, D, 2>(p, units, step, st);
+    case 4: return launch_quant_g<T, D, 4>(p, units, step, st);
+    default: return launch_quant_g<T, D, 8>(p, units, step, st);
+  }
+}
+
+}  // namespace kk

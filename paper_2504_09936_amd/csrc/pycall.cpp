@@ -17,6 +17,11 @@ struct Library {
   decltype(&keepkv_decode_step_static) decode_step_static;
   decltype(&keepkv_decode_attn) decode_attn;
   decltype(&keepkv_score) score;
+  decltype(&keepkv_decode_step_quant) decode_step_quant;
+  decltype(&keepkv_decode_attn_quant) decode_attn_quant;
+  decltype(&keepkv_append_quant) append_quant;
+  decltype(&keepkv_quantize) quantize;
+  decltype(&keepkv_dequantize) dequantize;
   PyObject *raw_stream, *device;                     // current stream's handle of a device, current device
   PyObject* argument_error;                          // what an argument of the wrong type raises
 };
@@ -24,10 +29,11 @@ const char kLibrary[] = "keepkv library";
 const Library* library_of(PyObject* self) { return static_cast<const Library*>(PyCapsule_GetPointer(self, kLibrary)); }
 
 enum Name { kBatch, kQHeads, kKvHeads, kHeadDim, kDtype, kScale, kK, kV, kVotes, kLogS, kBorn, kTObs, kLen, kCapacity, kLenHint,
-            kPlanSlots, kPlanWaves, kDataPtr, kNumel, kElementSize, kNames };
+            kPlanSlots, kPlanWaves, kDataPtr, kNumel, kElementSize,
+            kKScale, kVScale, kNames };
 const char* const kText[kNames] = {"batch", "n_q_heads", "n_kv_heads", "head_dim", "dtype", "scale", "k", "v", "votes", "log_s",
                                    "born", "t_obs", "len", "capacity", "len_hint", "plan_slots_per_split", "plan_wavefronts",
-                                   "data_ptr", "numel", "element_size"};
+                                   "data_ptr", "numel", "element_size", "k_scale", "v_scale"};
 PyObject* g_names[kNames];
 
 // Each returns false with a Python exception set.
@@ -94,6 +100,11 @@ bool float_argument(const Library* lib, PyObject* v, float* out) {
   if (PyErr_ExceptionMatches(PyExc_TypeError)) PyErr_Format(lib->argument_error, "float expected instead of %.80s instance", Py_TYPE(v)->tp_name);
   return false;
 }
+bool int_argument(const Library* lib, PyObject* v, int32_t* out) {
+  if (to_i32(v, out)) return true;
+  if (PyErr_ExceptionMatches(PyExc_TypeError)) PyErr_Format(lib->argument_error, "int expected instead of %.80s instance", Py_TYPE(v)->tp_name);
+  return false;
+}
 bool tensor_field(PyObject* obj, Name name, void** out) {
   PyObject* t = PyObject_GetAttr(obj, g_names[name]);
   const bool ok = t && address(t, PyExc_TypeError, out);
@@ -115,6 +126,10 @@ bool cache_of(PyObject* obj, keepkv_cache* c) {
          tensor_field(obj, kTObs, reinterpret_cast<void**>(&c->t_obs)) && tensor_field(obj, kLen, reinterpret_cast<void**>(&c->len)) &&
          int_field(obj, kCapacity, &c->capacity) && converted_int_field(obj, kLenHint, &c->len_hint) &&
          converted_int_field(obj, kPlanSlots, &c->plan_slots_per_split) && converted_int_field(obj, kPlanWaves, &c->plan_wavefronts);
+}
+bool quant_cache_of(PyObject* obj, keepkv_quant_cache* c) {
+  return cache_of(obj, &c->c) && tensor_field(obj, kKScale, reinterpret_cast<void**>(&c->k_scale)) &&
+         tensor_field(obj, kVScale, reinterpret_cast<void**>(&c->v_scale));
 }
 bool current_stream(const Library* lib, void** out) {
   PyObject* device = PyObject_CallNoArgs(lib->device);
@@ -201,6 +216,84 @@ PyObject* score(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   return status_of([&] { return lib->score(&L, &c, static_cast<const float*>(logits), alpha, stream); });
 }
 
+// as decode_step, on a cache of codes
+PyObject* decode_step_quant(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  const Library* lib = library_of(self);
+  keepkv_layout L;
+  keepkv_quant_cache c;
+  void *q, *k_t, *v_t, *out, *logits, *overflow, *ws, *stream;
+  float alpha;
+  size_t ws_bytes;
+  if (!lib || !arity("decode_step_quant", n, 10) || !layout_of(a[0], &L) || !quant_cache_of(a[1], &c) || !address_or_null(lib, a[2], &q) ||
+      !address_or_null(lib, a[3], &k_t) || !address_or_null(lib, a[4], &v_t) || !address_or_null(lib, a[5], &out) || !address_or_null(lib, a[6], &logits) ||
+      !float_argument(lib, a[7], &alpha) || !address_or_null(lib, a[8], &overflow) || !address_or_null(lib, a[9], &ws) || !bytes_of(lib, a[9], &ws_bytes) ||
+      !current_stream(lib, &stream))
+    return nullptr;
+  return status_of([&] {
+    return lib->decode_step_quant(&L, &c, q, k_t, v_t, out, static_cast<float*>(logits), alpha, static_cast<int32_t*>(overflow), ws, ws_bytes, stream);
+  });
+}
+
+// as decode_attn, on a cache of codes
+PyObject* decode_attn_quant(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  const Library* lib = library_of(self);
+  keepkv_layout L;
+  keepkv_quant_cache c;
+  void *q, *out, *logits, *lse, *ws, *stream;
+  size_t ws_bytes;
+  if (!lib || !arity("decode_attn_quant", n, 7) || !layout_of(a[0], &L) || !quant_cache_of(a[1], &c) || !address_or_null(lib, a[2], &q) ||
+      !address_or_null(lib, a[3], &out) || !address_or_null(lib, a[4], &logits) || !address_or_null(lib, a[5], &lse) || !address_or_null(lib, a[6], &ws) ||
+      !bytes_of(lib, a[6], &ws_bytes) || !current_stream(lib, &stream))
+    return nullptr;
+  return status_of([&] {
+    return lib->decode_attn_quant(&L, &c, q, out, static_cast<float*>(logits), static_cast<float*>(lse), ws, ws_bytes, stream);
+  });
+}
+
+// (layout, cache, k_t, v_t, n_tokens, counts, overflow)
+PyObject* append_quant(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  const Library* lib = library_of(self);
+  keepkv_layout L;
+  keepkv_quant_cache c;
+  void *k_t, *v_t, *counts, *overflow, *stream;
+  int32_t tokens;
+  if (!lib || !arity("append_quant", n, 7) || !layout_of(a[0], &L) || !quant_cache_of(a[1], &c) || !address_or_null(lib, a[2], &k_t) ||
+      !address_or_null(lib, a[3], &v_t) || !int_argument(lib, a[4], &tokens) || !address_or_null(lib, a[5], &counts) ||
+      !address_or_null(lib, a[6], &overflow) || !current_stream(lib, &stream))
+    return nullptr;
+  return status_of([&] {
+    return lib->append_quant(&L, &c, k_t, v_t, tokens, static_cast<const int32_t*>(counts), static_cast<int32_t*>(overflow), stream);
+  });
+}
+
+// (layout, cache of rows, cache of codes)
+PyObject* quantize(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  const Library* lib = library_of(self);
+  keepkv_layout L;
+  keepkv_cache rows;
+  keepkv_quant_cache codes;
+  void* stream;
+  if (!lib || !arity("quantize", n, 3) || !layout_of(a[0], &L) || !cache_of(a[1], &rows) || !quant_cache_of(a[2], &codes) ||
+      !current_stream(lib, &stream))
+    return nullptr;
+  return status_of([&] { return lib->quantize(&L, &rows, &codes, stream); });
+}
+
+// (layout, cache of codes, cache of rows)
+PyObject* dequantize(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  const Library* lib = library_of(self);
+  keepkv_layout L;
+  keepkv_cache rows;
+  keepkv_quant_cache codes;
+  void* stream;
+  if (!lib || !arity("dequantize", n, 3) || !layout_of(a[0], &L) || !quant_cache_of(a[1], &codes) || !cache_of(a[2], &rows) ||
+      !current_stream(lib, &stream))
+    return nullptr;
+  return status_of([&] { return lib->dequantize(&L, &codes, &rows, stream); });
+}
+
+#define KK_CALL(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
+PyMethodDef kQuantCalls[] = {KK_CALL(decode_step_quant), KK_CALL(decode_attn_quant), KK_CALL(append_quant), KK_CALL(quantize), KK_CALL(dequantize)};
 PyMethodDef kCalls[] = {
     {"decode_step", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(decode_step)), METH_FASTCALL, nullptr},
     {"decode_step_static", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(decode_step_static)), METH_FASTCALL, nullptr},
@@ -215,28 +308,20 @@ void release(PyObject* capsule) {
   delete lib;
 }
 
-// (raw_stream, device, argument_error, addresses of keepkv_decode_step, keepkv_decode_step_static, keepkv_decode_attn, keepkv_score):
-// these four functions for the library that the binding has loaded
-PyObject* bind(PyObject*, PyObject* args) {
-  unsigned long long f[4];
-  PyObject *raw_stream, *device, *argument_error;
-  if (!PyArg_ParseTuple(args, "OOOKKKK", &raw_stream, &device, &argument_error, &f[0], &f[1], &f[2], &f[3])) return nullptr;
-  Library* lib = new (std::nothrow) Library{reinterpret_cast<decltype(&keepkv_decode_step)>(f[0]),
-                                            reinterpret_cast<decltype(&keepkv_decode_step_static)>(f[1]),
-                                            reinterpret_cast<decltype(&keepkv_decode_attn)>(f[2]),
-                                            reinterpret_cast<decltype(&keepkv_score)>(f[3]), raw_stream, device, argument_error};
+// A tuple of the functions for a library; takes `lib` (null: no memory).
+PyObject* functions_of(Library* lib, PyMethodDef* defs, int n) {
   if (!lib) return PyErr_NoMemory();
   PyObject* capsule = PyCapsule_New(lib, kLibrary, release);
   if (!capsule) {
     delete lib;
     return nullptr;
   }
-  Py_INCREF(raw_stream);
-  Py_INCREF(device);
-  Py_INCREF(argument_error);
-  PyObject* calls = PyTuple_New(4);
-  for (int i = 0; calls && i < 4; ++i) {
-    PyObject* call = PyCFunction_New(&kCalls[i], capsule);     // (holds the capsule)
+  Py_INCREF(lib->raw_stream);
+  Py_INCREF(lib->device);
+  Py_INCREF(lib->argument_error);
+  PyObject* calls = PyTuple_New(n);
+  for (int i = 0; calls && i < n; ++i) {
+    PyObject* call = PyCFunction_New(&defs[i], capsule);       // (holds the capsule)
     if (call) PyTuple_SET_ITEM(calls, i, call);
     else Py_CLEAR(calls);
   }
@@ -244,7 +329,46 @@ PyObject* bind(PyObject*, PyObject* args) {
   return calls;
 }
 
-PyMethodDef kMethods[] = {{"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+// (raw_stream, device, argument_error, addresses of keepkv_decode_step, keepkv_decode_step_static, keepkv_decode_attn, keepkv_score):
+// these four functions for the library that the binding has loaded
+PyObject* bind(PyObject*, PyObject* args) {
+  unsigned long long f[4];
+  PyObject *raw_stream, *device, *argument_error;
+  if (!PyArg_ParseTuple(args, "OOOKKKK", &raw_stream, &device, &argument_error, &f[0], &f[1], &f[2], &f[3])) return nullptr;
+  Library* lib = new (std::nothrow) Library{};
+  if (lib) {
+    lib->decode_step = reinterpret_cast<decltype(&keepkv_decode_step)>(f[0]);
+    lib->decode_step_static = reinterpret_cast<decltype(&keepkv_decode_step_static)>(f[1]);
+    lib->decode_attn = reinterpret_cast<decltype(&keepkv_decode_attn)>(f[2]);
+    lib->score = reinterpret_cast<decltype(&keepkv_score)>(f[3]);
+    lib->raw_stream = raw_stream;
+    lib->device = device;
+    lib->argument_error = argument_error;
+  }
+  return functions_of(lib, kCalls, 4);
+}
+
+// (raw_stream, device, argument_error, addresses of keepkv_decode_step_quant, keepkv_decode_attn_quant, keepkv_append_quant,
+// keepkv_quantize, keepkv_dequantize): these five
+PyObject* bind_quant(PyObject*, PyObject* args) {
+  unsigned long long f[5];
+  PyObject *raw_stream, *device, *argument_error;
+  if (!PyArg_ParseTuple(args, "OOOKKKKK", &raw_stream, &device, &argument_error, &f[0], &f[1], &f[2], &f[3], &f[4])) return nullptr;
+  Library* lib = new (std::nothrow) Library{};
+  if (lib) {
+    lib->decode_step_quant = reinterpret_cast<decltype(&keepkv_decode_step_quant)>(f[0]);
+    lib->decode_attn_quant = reinterpret_cast<decltype(&keepkv_decode_attn_quant)>(f[1]);
+    lib->append_quant = reinterpret_cast<decltype(&keepkv_append_quant)>(f[2]);
+    lib->quantize = reinterpret_cast<decltype(&keepkv_quantize)>(f[3]);
+    lib->dequantize = reinterpret_cast<decltype(&keepkv_dequantize)>(f[4]);
+    lib->raw_stream = raw_stream;
+    lib->device = device;
+    lib->argument_error = argument_error;
+  }
+  return functions_of(lib, kQuantCalls, 5);
+}
+
+PyMethodDef kMethods[] = {{"bind", bind, METH_VARARGS, nullptr}, {"bind_quant", bind_quant, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_pycall", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
