@@ -37,13 +37,20 @@ __device__ __forceinline__ bf16x8_t expand8(uint32_t lo, uint32_t hi, float scal
   return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-__device__ __forceinline__ float uniform_f32(float x) {
-  return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+// Two reads of 16 bytes from LDS that the compiler does not order behind outstanding copies into it.
+template <typename V>
+__device__ __forceinline__ void lds_read2(uint32_t at0, uint32_t at1, V& x0, V& x1) {
+  asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %3\n\ts_waitcnt lgkmcnt(0)" : "=&v"(x0), "=&v"(x1) : "v"(at0), "v"(at1) : "memory");
 }
 
-// LDS of a wavefront: kBuffers V tiles, later its deposit (and the weights of the splits behind it).
+// LDS of a wavefront: V tiles and the query rows (whole kilobytes), later its deposit (and the weights of the splits behind it).
+template <typename T>
+constexpr int quant_q_bytes(int D, int G) {
+  return (G * D * (int)sizeof(T) + 1023) / 1024 * 1024;
+}
+template <typename T>
 constexpr int quant_wave_bytes(int D, int G, int buffers) {
-  const int tiles = buffers * kQBlock * D, deposit = (G * D + 16 + 128) * 4;
+  const int tiles = buffers * kQBlock * D + quant_q_bytes<T>(D, G), deposit = (G * D + 16 + 128) * 4;
   return (tiles > deposit ? tiles : deposit + 127) / 128 * 128;
 }
 constexpr int kStageSlots = 256;                 // of a wavefront: new scores that wait in LDS for the end of a tile loop
@@ -61,7 +68,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
   constexpr int TILE_BYTES = kQBlock * D, VLOADS = TILE_BYTES / (kWave * 16);
   constexpr int NV = kShare<G>;
   constexpr int kBuffers = kTiles == kOne ? 1 : 2;
-  constexpr int WAVE_BYTES = quant_wave_bytes(D, G, kBuffers);
+  constexpr int WAVE_BYTES = quant_wave_bytes<T>(D, G, kBuffers);
   constexpr int QTERMS = kF32 ? 3 : 1;
   constexpr int REQUESTS = 2 * KH + 2 + (STEP ? 1 : 0) + VLOADS;      // of a tile
   constexpr int EPL = D / kWave;                 // channels of a lane in an appended row
@@ -74,6 +81,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
   const int split = kMayShareXcd ? blockIdx.y : blockIdx.x;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, q = lane >> 4;
+  KK_TS(0);
   const int len_old = p.len[unit];
   const int t_old = STEP ? p.t_obs[unit] : 0;
   const int start = split * p.per;
@@ -100,29 +108,6 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
     __hip_atomic_fetch_add(&p.arrivals[unit], 1ull << (8 * xcd_id()), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 
   // ---- requests
-  bf16x8_t qb[QTERMS][KS];                       // column l16 is head l16 mod G, this lane's channels 64 h + 16 q + 8 t + j of k-step 2 h + t
-  {
-    const T* qrow = reinterpret_cast<const T*>(p.q) + ((size_t)unit * G + g_l) * D + 16 * q;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const T* at = qrow + 64 * (ks >> 1) + 8 * (ks & 1);
-      if constexpr (!kF32) {
-        qb[0][ks] = *reinterpret_cast<const bf16x8_t*>(at);
-      } else {
-        const float4 a = *reinterpret_cast<const float4*>(at), b = *reinterpret_cast<const float4*>(at + 4);
-        float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-        for (int t = 0; t < 3; ++t) {            // each term takes the 8 leading bits of what is left
-          uint32_t w[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = pack_hi16(x[2 * i], x[2 * i + 1]);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] -= __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x[i]) & 0xFFFF0000u);
-          qb[t][ks] = __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
-        }
-      }
-    }
-  }
   float k_new[EPL], v_new[EPL];                  // STEP: this lane's channels EPL lane .. of the token
   if constexpr (STEP) {
 #pragma unroll
@@ -132,6 +117,17 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
       v_new[e] = kF32 ? reinterpret_cast<const float*>(p.v_t)[at] : bf16_to_f32(reinterpret_cast<const uint16_t*>(p.v_t)[at]);
     }
   }
+  // The query rows go through LDS: gathered by the lanes that need them they would be 16 / G times their bytes.  Chunk c of head g sits at
+  // position c ^ (g mod 8) of its row.
+  unsigned char* const s_q = Tb + kBuffers * TILE_BYTES;
+  constexpr int QROW = D * (int)sizeof(T), QCHUNKS = QROW / 16;
+#pragma unroll
+  for (int j = 0; j < quant_q_bytes<T>(D, G) / 1024; ++j) {
+    const int c = min(j * kWave + lane, G * QCHUNKS - 1), g = c / QCHUNKS;       // surplus lanes repeat the last chunk
+    copy_to_lds<0>(reinterpret_cast<const unsigned char*>(p.q) + (size_t)unit * G * QROW, (size_t)G * QROW, s_q + j * 1024,
+                   (uint32_t)((c ^ (g & 7)) * 16), 0);
+  }
+  __builtin_amdgcn_sched_barrier(0);
   struct Tile {
     u32x4_t k[2][KH];
     float scale;                                 // of K in even lanes, of V in odd ones
@@ -156,6 +152,35 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
       copy_to_lds<2>(vbytes, (size_t)(last_row + 1) * D, buf + i * (kWave * 16), (uint32_t)(min(tbase + row, last_row) * D + 16 * chunk), 0);
     }
     __builtin_amdgcn_sched_barrier(0);
+  };
+
+  // Column l16 of the B operand is head l16 mod G, of k-step 2 h + t this lane's channels 64 h + 16 q + 8 t + j; f32 queries in three terms.
+  bf16x8_t qb[QTERMS][KS];
+  auto read_q = [&](auto behind) {               // with at most `behind` requests outstanding the copies have landed
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(behind)::value) : "memory");
+    const uint32_t row = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)(s_q + g_l * QROW);
+    auto chunk = [&](int c) { return row + (uint32_t)((c ^ (g_l & 7)) * 16); };
+    if constexpr (!kF32) {
+      lds_read2(chunk(2 * q), chunk(2 * q + 1), qb[0][0], qb[0][1]);
+      if constexpr (KS == 4) lds_read2(chunk(8 + 2 * q), chunk(9 + 2 * q), qb[0][2], qb[0][3]);
+    } else {
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        f32x4_t a, b;
+        const int c = 16 * (ks >> 1) + 4 * q + 2 * (ks & 1);
+        lds_read2(chunk(c), chunk(c + 1), a, b);
+        float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+#pragma unroll
+        for (int t = 0; t < 3; ++t) {            // each term takes the 8 leading bits of what is left
+          uint32_t w[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] = pack_hi16(x[2 * i], x[2 * i + 1]);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] -= __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x[i]) & 0xFFFF0000u);
+          qb[t][ks] = __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
+        }
+      }
+    }
   };
 
   const bool grow = STEP && len_old < p.capacity;
@@ -355,7 +380,8 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
   const bool staged = kTiles == kLoop && STEP && p.per <= kWaves * kStageSlots;
   constexpr int kTileStep = kWaves * kQBlock;
   constexpr std::integral_constant<int, 0> kAll{};
-  constexpr std::integral_constant<int, REQUESTS> kFirst{};
+  constexpr std::integral_constant<int, REQUESTS> kFirst{};           // (a tile's)
+  constexpr std::integral_constant<int, 2 * REQUESTS> kBoth{};
   const int base = start + wave * kQBlock;
   bool own0 = false, own1 = false;               // results per slot that are stored at the very end
   float x0 = 0.f, x1 = 0.f, ls0 = 0.f, ls1 = 0.f;
@@ -363,12 +389,14 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
   if constexpr (kTiles == kOne) {
     if (base < lim) {
       request(base, t0, Tb);
+      read_q(kFirst);
       own0 = compute(base, t0, Tb, true, kAll, x0, ls0);
     }
   } else if constexpr (kTiles == kTwo) {
     if (base < lim) {
       request(base, t0, Tb);
       request(base + kTileStep, t1, Tb + TILE_BYTES);                 // (beyond the last row its rows are the last row's)
+      read_q(kBoth);
       own0 = compute(base, t0, Tb, true, kFirst, x0, ls0);
       if (base + kTileStep < lim) own1 = compute(base + kTileStep, t1, Tb + TILE_BYTES, false, kAll, x1, ls1);
     }
@@ -391,6 +419,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
     if (base < lim) {
       request(base, t0, Tb);
       request(base + kTileStep, t1, Tb + TILE_BYTES);
+      read_q(kBoth);
     }
     for (int tb = base; tb < lim; tb += 2 * kTileStep) {
       float x, ls;
@@ -408,6 +437,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                  // no copy may land in what follows
   }
 
+  KK_TS(1);
   // ---- this wavefront's state, then the workgroup's
   const float l_tot = over_head_lanes<G>(l_run, [](float a, float b) { return a + b; });
   constexpr int kPartStride = WAVE_BYTES / 4;
@@ -421,6 +451,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
   }
   if constexpr (kTiles == kLoop && STEP) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the staged scores are in LDS
   __syncthreads();
+  KK_TS(2);
   if constexpr (kTiles != kLoop) {
     auto store = [&](int tbase, bool mine, float x, float ls_old) {
       const size_t at = ubase + tbase + row_mine;
@@ -456,7 +487,7 @@ template <typename T, int D, int G>
 keepkv_status launch_quant_g(const QuantParams& p, int units, bool step, hipStream_t st) {
   auto go = [&](auto step_tag, auto tiles_tag, auto meet_tag, auto waves_tag) -> keepkv_status {
     constexpr int kTiles = decltype(tiles_tag)::value, kWaves = decltype(waves_tag)::value;
-    constexpr size_t lds = (size_t)kWaves * (quant_wave_bytes(D, G, kTiles == kOne ? 1 : 2) + (kTiles == kLoop ? kStageSlots * 4 : 0));
+    constexpr size_t lds = (size_t)kWaves * (quant_wave_bytes<T>(D, G, kTiles == kOne ? 1 : 2) + (kTiles == kLoop ? kStageSlots * 4 : 0));
     auto* kernel = decode_quant_kernel<T, D, G, decltype(step_tag)::value, kTiles, decltype(meet_tag)::value, kWaves>;
     if constexpr (lds > 60 * 1024) {
       static const bool allowed = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) == hipSuccess;

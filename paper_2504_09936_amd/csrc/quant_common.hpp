@@ -27,11 +27,14 @@ __device__ __forceinline__ uint32_t finite_magnitude(float x) {
   return u < 0x7F800000u ? u : 0u;
 }
 
-// Two, four f32 (already divided by the scale) as codes, to nearest even; what is not finite becomes NaN.
+// Four f32 (already divided by the scale) as codes, to nearest even; encode4: an infinity becomes NaN, encode4_no_inf: there is none.
+__device__ __forceinline__ uint32_t encode4_no_inf(float a, float b, float c, float d) {
+  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
+}
 __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) {
   auto nan_if_inf = [](float x) { return __builtin_fabsf(x) == INFINITY ? __builtin_nanf("") : x; };
-  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(nan_if_inf(a), nan_if_inf(b), 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(nan_if_inf(c), nan_if_inf(d), lo, true);
+  return encode4_no_inf(nan_if_inf(a), nan_if_inf(b), nan_if_inf(c), nan_if_inf(d));
 }
 // Four codes as f32.
 __device__ __forceinline__ void decode4(uint32_t w, float (&x)[4]) {
@@ -46,7 +49,7 @@ __device__ __forceinline__ void decode4(uint32_t w, float (&x)[4]) {
 __device__ __forceinline__ uint32_t shift_codes(uint32_t w, float ratio) {
   float x[4];
   decode4(w, x);
-  return encode4(x[0] * ratio, x[1] * ratio, x[2] * ratio, x[3] * ratio);
+  return encode4_no_inf(x[0] * ratio, x[1] * ratio, x[2] * ratio, x[3] * ratio);
 }
 
 // maximum over the wavefront, in every lane
