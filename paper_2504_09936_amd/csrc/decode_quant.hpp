@@ -82,8 +82,10 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, q = lane >> 4;
   KK_TS(0);
-  const int len_old = p.len[unit];
-  const int t_old = STEP ? p.t_obs[unit] : 0;
+  // The head's words, requested first of all and awaited when the first tile has landed.  (Vector loads, which complete in order: a scalar
+  // load's wait would be for every scalar load, and a choice between len and the bound on it would wait before anything is requested.)
+  const int len_word = __hip_atomic_load(&p.len[unit], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  const int t_word = STEP ? __hip_atomic_load(&p.t_obs[unit], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) : 0;
   const int start = split * p.per;
   const size_t ubase = (size_t)unit * p.capacity;
   const int blocks = quant_blocks(p.capacity);
@@ -93,7 +95,9 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
   unsigned char* const Tb = smem_tiles + wave * WAVE_BYTES;
 
   // slots that may be read (len itself, or the caller's bound on it, so that nothing waits for len); tiles up to `lim`
-  const int bound = p.len_hint > 0 ? min(p.len_hint, p.capacity) : len_old;
+  int bound;
+  if (p.len_hint > 0) bound = min(p.len_hint, p.capacity);
+  else bound = __builtin_amdgcn_readfirstlane(len_word);
   const int lim = min(min(bound + (STEP ? 1 : 0), p.capacity), start + p.per);
   const int last_row = max(bound - 1, 0);
 
@@ -183,11 +187,16 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
     }
   };
 
-  const bool grow = STEP && len_old < p.capacity;
-  const int len = grow ? len_old + 1 : len_old;
-  const int live_end = min(len, start + p.per);
-  const int new_row = len_old % kQBlock;
-  const int own_base = grow ? len_old - new_row : -1;                 // the tile that the appended token joins
+  bool grow;
+  int len_old, len, live_end, new_row, own_base;                      // own_base: the tile that the appended token joins
+  auto read_len = [&]() {
+    len_old = __builtin_amdgcn_readfirstlane(len_word);
+    grow = STEP && len_old < p.capacity;
+    len = grow ? len_old + 1 : len_old;
+    live_end = min(len, start + p.per);
+    new_row = len_old % kQBlock;
+    own_base = grow ? len_old - new_row : -1;
+  };
 
   const float sl2 = p.scale * kLog2e;
   float m_run = kLowest, l_run = 0.f;
@@ -390,6 +399,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
     if (base < lim) {
       request(base, t0, Tb);
       read_q(kFirst);
+      read_len();
       own0 = compute(base, t0, Tb, true, kAll, x0, ls0);
     }
   } else if constexpr (kTiles == kTwo) {
@@ -397,6 +407,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
       request(base, t0, Tb);
       request(base + kTileStep, t1, Tb + TILE_BYTES);                 // (beyond the last row its rows are the last row's)
       read_q(kBoth);
+      read_len();
       own0 = compute(base, t0, Tb, true, kFirst, x0, ls0);
       if (base + kTileStep < lim) own1 = compute(base + kTileStep, t1, Tb + TILE_BYTES, false, kAll, x1, ls1);
     }
@@ -420,6 +431,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
       request(base, t0, Tb);
       request(base + kTileStep, t1, Tb + TILE_BYTES);
       read_q(kBoth);
+      read_len();
     }
     for (int tb = base; tb < lim; tb += 2 * kTileStep) {
       float x, ls;
@@ -438,6 +450,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
   }
 
   KK_TS(1);
+  read_len();                                    // (a wavefront without a tile)
   // ---- this wavefront's state, then the workgroup's
   const float l_tot = over_head_lanes<G>(l_run, [](float a, float b) { return a + b; });
   constexpr int kPartStride = WAVE_BYTES / 4;
@@ -473,13 +486,13 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
     }
     if (lane == 0) {
       p.votes[ubase + len_old] = 1;
-      p.born[ubase + len_old] = t_old;
+      p.born[ubase + len_old] = t_word;
       qp.k_scale[(size_t)unit * blocks + len_old / kQBlock] = __builtin_bit_cast(float, new_ks);
       qp.v_scale[(size_t)unit * blocks + len_old / kQBlock] = __builtin_bit_cast(float, new_vs);
     }
   }
   combine_and_finish<T, D, G, kWaves, STEP, kWaves, true, kMeet == kSoloMeet, kMayShareXcd>(p, s_ml, s_ml + G, s_acc, kPartStride, kPartStride, &s_last,
-                                                                                             unit, split, grow, len, t_old,
+                                                                                             unit, split, grow, len, t_word,
                                                                                              __builtin_amdgcn_readfirstlane(s_one_xcd) != 0);
 }
 
