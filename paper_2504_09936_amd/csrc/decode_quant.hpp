@@ -233,15 +233,15 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
 
   // One tile; V has landed when at most v_wait requests are outstanding.  Returns the group-mean logit of slot row_mine and whether this lane
   // stores it.
-  // first: no tile of this wavefront has been computed.
-  auto compute = [&](int tbase, Tile& t, unsigned char* Vb, bool first, auto v_wait, float& x_out, float& ls_old) -> bool {
+  // first: no tile of this wavefront has been computed.  may_own: the appended token may join it (only a wavefront's last live tile).
+  auto compute = [&](int tbase, Tile& t, unsigned char* Vb, bool first, auto may_own, auto v_wait, float& x_out, float& ls_old) -> bool {
     constexpr int kVWait = decltype(v_wait)::value;
     const int n_live = min(kQBlock, live_end - tbase);
     x_out = ls_old = 0.f;
     if (n_live <= 0) return false;               // uniform: below the caller's bound but dead, its scales mean nothing
     float ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, t.scale), 0));
     float vs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, t.scale), 1));
-    const bool own = STEP && tbase == own_base;  // uniform
+    const bool own = STEP && decltype(may_own)::value && tbase == own_base;   // uniform
     bool v_moves = false;
     float v_ratio = 1.f;
     if (own) {
@@ -388,6 +388,8 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
   unsigned char* const s_stage = smem_tiles + kWaves * WAVE_BYTES;
   const bool staged = kTiles == kLoop && STEP && p.per <= kWaves * kStageSlots;
   constexpr int kTileStep = kWaves * kQBlock;
+  constexpr std::true_type kMayOwn{};
+  constexpr std::false_type kNotLast{};
   constexpr std::integral_constant<int, 0> kAll{};
   constexpr std::integral_constant<int, REQUESTS> kFirst{};           // (a tile's)
   constexpr std::integral_constant<int, 2 * REQUESTS> kBoth{};
@@ -400,7 +402,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
       request(base, t0, Tb);
       read_q(kFirst);
       read_len();
-      own0 = compute(base, t0, Tb, true, kAll, x0, ls0);
+      own0 = compute(base, t0, Tb, true, kMayOwn, kAll, x0, ls0);
     }
   } else if constexpr (kTiles == kTwo) {
     if (base < lim) {
@@ -408,8 +410,8 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
       request(base + kTileStep, t1, Tb + TILE_BYTES);                 // (beyond the last row its rows are the last row's)
       read_q(kBoth);
       read_len();
-      own0 = compute(base, t0, Tb, true, kFirst, x0, ls0);
-      if (base + kTileStep < lim) own1 = compute(base + kTileStep, t1, Tb + TILE_BYTES, false, kAll, x1, ls1);
+      own0 = compute(base, t0, Tb, true, kMayOwn, kFirst, x0, ls0);
+      if (base + kTileStep < live_end) own1 = compute(base + kTileStep, t1, Tb + TILE_BYTES, false, kMayOwn, kAll, x1, ls1);
     }
   } else {
     auto publish = [&](int tbase, bool mine, float x, float ls_old) {
@@ -426,25 +428,37 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
         }
       }
     };
-    // two tiles in flight: a tile's buffer is requested again when it has been used (beyond the last row: the last row again)
+    // Two tiles in flight: a tile's buffer is requested again when it has been used, if a tile is left for it.  The ways out are written
+    // out, so that on each the number of requests behind a tile is known and none is made for nothing: a surplus one is a memory
+    // round trip before the wavefront may deposit (40 heads of D 64 x 2892 slots in splits of three tiles 11.0 us with, 8.9 without).
     if (base < lim) {
       request(base, t0, Tb);
-      request(base + kTileStep, t1, Tb + TILE_BYTES);
+      request(base + kTileStep, t1, Tb + TILE_BYTES);                 // (beyond the last row its rows are the last row's)
       read_q(kBoth);
       read_len();
-    }
-    for (int tb = base; tb < lim; tb += 2 * kTileStep) {
-      float x, ls;
-      bool mine = compute(tb, t0, Tb, tb == base, kFirst, x, ls);
-      publish(tb, mine, x, ls);
-      __builtin_amdgcn_sched_barrier(0);
-      request(tb + 2 * kTileStep, t0, Tb);
-      if (tb + kTileStep < lim) {
-        mine = compute(tb + kTileStep, t1, Tb + TILE_BYTES, false, kFirst, x, ls);
-        publish(tb + kTileStep, mine, x, ls);
+      auto tile = [&](int tb, Tile& t, unsigned char* Vb, auto may_own, auto v_wait) {
+        float x, ls;
+        const bool mine = compute(tb, t, Vb, tb == base, may_own, v_wait, x, ls);
+        publish(tb, mine, x, ls);
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      int tb = base, left = live_end > base ? (live_end - base + kTileStep - 1) / kTileStep : 0;
+      while (left > 2) {
+        tile(tb, t0, Tb, kNotLast, kFirst);
+        request(tb + 2 * kTileStep, t0, Tb);
+        if (left == 3) {
+          tile(tb + kTileStep, t1, Tb + TILE_BYTES, kNotLast, kFirst);
+          tile(tb + 2 * kTileStep, t0, Tb, kMayOwn, kAll);
+          left = 0;
+          break;
+        }
+        tile(tb + kTileStep, t1, Tb + TILE_BYTES, kNotLast, kFirst);
+        request(tb + 3 * kTileStep, t1, Tb + TILE_BYTES);
+        tb += 2 * kTileStep;
+        left -= 2;
       }
-      __builtin_amdgcn_sched_barrier(0);
-      request(tb + 3 * kTileStep, t1, Tb + TILE_BYTES);
+      if (left > 0) tile(tb, t0, Tb, kMayOwn, kFirst);
+      if (left > 1) tile(tb + kTileStep, t1, Tb + TILE_BYTES, kMayOwn, kAll);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                  // no copy may land in what follows
   }
