@@ -14,7 +14,7 @@ void choose_split_quant(const keepkv_layout* L, int capacity, long& per, int& wa
   const double slot_bytes = 2.0 * L->head_dim + 20.0;
   const long max_ns = (capacity + kMinQuantSplit - 1) / kMinQuantSplit;
   double best = 1e300;
-  for (int wv = 4; wv <= 8; wv += 4) {
+  for (int wv = 4; wv <= (L->dtype == KEEPKV_F32 ? 4 : 8); wv += 4) {
     const double res_max = 256.0 * (8 / wv);
     for (long ns = 1; ns <= max_ns && (ns == 1 || units * (double)ns <= kMaxQuantWorkgroups); ++ns) {
       long cand = ((capacity + ns - 1) / ns + kQBlock - 1) / kQBlock * kQBlock;
@@ -53,6 +53,7 @@ DecodePlan make_quant_plan(const keepkv_layout* L, int capacity, int force_per, 
   int waves = 4;
   choose_split_quant(L, capacity, per, waves);
   if (force_waves > 0) waves = force_waves;
+  if (L->dtype == KEEPKV_F32) waves = 4;
   if (force_per >= 64) per = force_per / kQBlock * kQBlock;
   long ns = (capacity + per - 1) / per;
   if (ns > 1024) { ns = 1024; per = ((capacity + ns - 1) / ns + 63) / 64 * 64; ns = (capacity + per - 1) / per; }

@@ -16,18 +16,22 @@ namespace {
 // bf16 operands): a code times its scale has 4 significant bits, so it is exact in bf16, and the conversion instruction applies the scale.
 // The query stays as it is (f32 queries as three bf16 terms, 24 bits) and products are summed in f32.
 //
-// K rows travel straight into registers in the layout of the A operand: the sum over channels may run in any order, so lane (row l16,
-// quarter q) takes the 16 bytes at 64 h + 16 q (h = 0, 1) and the queries are read in that order.  V rows go to LDS by asynchronous
-// copies, and ds_read_b64_tr_b8 returns a channel's 8 slots of a lane in the order in which the scores lie (checked on
-// the device).  16-byte chunk c of row r sits at position c ^ swizzle(r), so that the 8 rows of a transposed read lie in different banks.
+// K and V rows go to LDS by asynchronous copies of whole kilobytes.  (K rows loaded straight into the operand's registers, 64 bytes of a
+// row at a time, streamed 13 % slower: 221 MB in 40.9 us, 35.9 so.)  A K operand is read in an order of the channels that suits 16-byte
+// reads -- the sum over channels may run in any: lane (row l16, quarter q) takes the 16 bytes at 64 h + 16 q (h = 0, 1), and the queries
+// are read alike.  Of V, ds_read_b64_tr_b8 returns a channel's 8 slots of a lane in the order in which the scores lie (checked on the
+// device).  16-byte chunk c of row r sits at position c ^ swizzle(r), so that what is read at once lies in different banks: 8 rows in
+// sequence of K, rows 4 q + i and 16 + 4 q + i of V.
 //
 // The appended token is a row of the block that its slot lies in, so the wavefront of that tile quantises it, moves the block's codes to a
-// larger scale if the token needs one (in registers and LDS, and back to memory), and puts the row in before the products.  No other wavefront
-// reads that block.
+// larger scale if the token needs one (in LDS, and back to memory), and puts the row in before the products.  No other wavefront
+// reads that block.  What the row needs of the scale is worked out by every wavefront while its first tile travels: by the one
+// alone, when the tile had landed, 8 heads x 852 slots took 6.54 us, 6.28 so.
 template <int D>
 __device__ __forceinline__ int swizzle(int row) {
-  if constexpr (D == 128) return (row & 3) | ((row >> 4) & 1) << 2;   // rows of 128 bytes: 4 q + i and 16 + 4 q + i apart
-  else return ((row >> 1) & 1) | ((row >> 4) & 1) << 1;               // two rows to 128 bytes
+  const int half = ((row >> 2) ^ (row >> 4)) & 1;
+  if constexpr (D == 128) return (row & 3) | half << 2;
+  else return ((row >> 1) & 1) | half << 1;                           // (two rows to 128 bytes)
 }
 
 // 8 codes (two words) times the scale, in bf16: exact
@@ -43,17 +47,31 @@ __device__ __forceinline__ void lds_read2(uint32_t at0, uint32_t at1, V& x0, V& 
   asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %3\n\ts_waitcnt lgkmcnt(0)" : "=&v"(x0), "=&v"(x1) : "v"(at0), "v"(at1) : "memory");
 }
 
-// LDS of a wavefront: V tiles and the query rows (whole kilobytes), later its deposit (and the weights of the splits behind it).
+// Four such reads.
+template <typename V>
+__device__ __forceinline__ void lds_read4(const uint32_t (&at)[4], V (&x)[4]) {
+  asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %6\n\tds_read_b128 %3, %7\n\ts_waitcnt lgkmcnt(0)"
+               : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3])
+               : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3])
+               : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p; }
+
+// LDS of a wavefront: K and V tiles and the query rows (whole kilobytes), later its deposit (and the weights of the splits behind it).
 template <typename T>
 constexpr int quant_q_bytes(int D, int G) {
   return (G * D * (int)sizeof(T) + 1023) / 1024 * 1024;
 }
 template <typename T>
 constexpr int quant_wave_bytes(int D, int G, int buffers) {
-  const int tiles = buffers * kQBlock * D + quant_q_bytes<T>(D, G), deposit = (G * D + 16 + 128) * 4;
+  const int tiles = buffers * 2 * kQBlock * D + quant_q_bytes<T>(D, G), deposit = (G * D + 16 + 128) * 4;
   return (tiles > deposit ? tiles : deposit + 127) / 128 * 128;
 }
-constexpr int kStageSlots = 256;                 // of a wavefront: new scores that wait in LDS for the end of a tile loop
+// New scores that wait in LDS for the end of a tile loop: each wavefront's where its query rows were.
+template <typename T>
+constexpr int quant_stage_slots(int D, int G) {
+  return quant_q_bytes<T>(D, G) / 4;
+}
 
 // How many tiles a wavefront has at most: one, two (all requested before the first wait), more (a loop over two buffers); and where splits
 // meet: not at all, through memory, or within an XCD where their workgroups find that they may.
@@ -65,17 +83,16 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
   const DecodeParams& p = qp.d;
   constexpr bool kF32 = sizeof(T) == 4;
   constexpr int KH = D / 64, KS = D / 32, NTILE = D / 16, CHUNKS = D / 16;
-  constexpr int TILE_BYTES = kQBlock * D, VLOADS = TILE_BYTES / (kWave * 16);
+  constexpr int TILE_BYTES = kQBlock * D, BUFFER = 2 * TILE_BYTES, VLOADS = TILE_BYTES / (kWave * 16);
   constexpr int NV = kShare<G>;
   constexpr int kBuffers = kTiles == kOne ? 1 : 2;
   constexpr int WAVE_BYTES = quant_wave_bytes<T>(D, G, kBuffers);
   constexpr int QTERMS = kF32 ? 3 : 1;
-  constexpr int REQUESTS = 2 * KH + 2 + (STEP ? 1 : 0) + VLOADS;      // of a tile
+  constexpr int REQUESTS = 2 * VLOADS + 2 + (STEP ? 1 : 0);           // of a tile
   constexpr int EPL = D / kWave;                 // channels of a lane in an appended row
   extern __shared__ __align__(256) unsigned char smem_tiles[];
   constexpr bool kMayShareXcd = kMeet == kXcdMeet;
   __shared__ int s_last, s_one_xcd;
-  __shared__ __align__(16) unsigned char s_new[2 * D];                // the appended token's codes: K, V
 
   const int unit = kMayShareXcd ? (int)(blockIdx.z * 8 + blockIdx.x) : (int)blockIdx.y;
   const int split = kMayShareXcd ? blockIdx.y : blockIdx.x;
@@ -123,7 +140,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
   }
   // The query rows go through LDS: gathered by the lanes that need them they would be 16 / G times their bytes.  Chunk c of head g sits at
   // position c ^ (g mod 8) of its row.
-  unsigned char* const s_q = Tb + kBuffers * TILE_BYTES;
+  unsigned char* const s_q = Tb + kBuffers * BUFFER;
   constexpr int QROW = D * (int)sizeof(T), QCHUNKS = QROW / 16;
 #pragma unroll
   for (int j = 0; j < quant_q_bytes<T>(D, G) / 1024; ++j) {
@@ -133,7 +150,6 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
   }
   __builtin_amdgcn_sched_barrier(0);
   struct Tile {
-    u32x4_t k[2][KH];
     float scale;                                 // of K in even lanes, of V in odd ones
     int votes;
     float ls;                                    // ln S of slot row_mine
@@ -144,17 +160,16 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
     t.votes = p.votes[ubase + at];
     if constexpr (STEP) t.ls = p.log_s[ubase + at];
     else t.ls = 0.f;
-#pragma unroll
-    for (int st = 0; st < 2; ++st) {
-      const uint32_t off = (uint32_t)(min(tbase + 16 * st + l16, last_row) * D + 16 * q);
-#pragma unroll
-      for (int h = 0; h < KH; ++h) t.k[st][h] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(kbytes + off + 64 * h));
-    }
+    uint32_t off[VLOADS];
 #pragma unroll
     for (int i = 0; i < VLOADS; ++i) {
       const int at16 = i * kWave + lane, row = at16 / CHUNKS, chunk = (at16 % CHUNKS) ^ swizzle<D>(row);
-      copy_to_lds<2>(vbytes, (size_t)(last_row + 1) * D, buf + i * (kWave * 16), (uint32_t)(min(tbase + row, last_row) * D + 16 * chunk), 0);
+      off[i] = (uint32_t)(min(tbase + row, last_row) * D + 16 * chunk);
     }
+#pragma unroll
+    for (int i = 0; i < VLOADS; ++i) copy_to_lds<2>(kbytes, (size_t)(last_row + 1) * D, buf + i * (kWave * 16), off[i], 0);
+#pragma unroll
+    for (int i = 0; i < VLOADS; ++i) copy_to_lds<2>(vbytes, (size_t)(last_row + 1) * D, buf + TILE_BYTES + i * (kWave * 16), off[i], 0);
     __builtin_amdgcn_sched_barrier(0);
   };
 
@@ -162,7 +177,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
   bf16x8_t qb[QTERMS][KS];
   auto read_q = [&](auto behind) {               // with at most `behind` requests outstanding the copies have landed
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(behind)::value) : "memory");
-    const uint32_t row = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)(s_q + g_l * QROW);
+    const uint32_t row = lds_address(s_q + g_l * QROW);
     auto chunk = [&](int c) { return row + (uint32_t)((c ^ (g_l & 7)) * 16); };
     if constexpr (!kF32) {
       lds_read2(chunk(2 * q), chunk(2 * q + 1), qb[0][0], qb[0][1]);
@@ -204,24 +219,24 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
 #pragma unroll
   for (int nt = 0; nt < NTILE; ++nt) O[nt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
-  auto scale_for = [&](const float (&x)[EPL], float old, uint32_t& bits) {   // of the block with the new row
-    float a = 0.f;
+  // The scales that the new rows need, worked out while the first tile travels.
+  uint32_t need_k = 0, need_v = 0;
+  auto read_new = [&]() {
+    auto need = [&](const float (&x)[EPL]) {
+      float a = 0.f;
 #pragma unroll
-    for (int e = 0; e < EPL; ++e) a = fmaxf(a, __builtin_bit_cast(float, finite_magnitude(x[e])));
-    a = over_head_lanes<1>(a, [](float u, float v) { return fmaxf(u, v); });
-    bits = scale_bits(__builtin_bit_cast(uint32_t, a));
-    const uint32_t had = __builtin_bit_cast(uint32_t, old);
-    if (new_row > 0) bits = max(bits, had);
-    bits = __builtin_amdgcn_readfirstlane(bits);
-    return new_row > 0 && bits != had;           // the live codes move to the larger scale
-  };
-  auto encode_row = [&](const float (&x)[EPL], uint32_t bits, unsigned char* at) {
-    const float inv = inverse_scale(bits);
-    if constexpr (EPL == 2) *reinterpret_cast<uint16_t*>(at + 2 * lane) = (uint16_t)encode4(x[0] * inv, x[1] * inv, 0.f, 0.f);
-    else at[lane] = (unsigned char)encode4(x[0] * inv, 0.f, 0.f, 0.f);
+      for (int e = 0; e < EPL; ++e) a = fmaxf(a, __builtin_bit_cast(float, finite_magnitude(x[e])));
+      a = over_head_lanes<1>(a, [](float u, float v) { return fmaxf(u, v); });
+      return scale_bits((uint32_t)__builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, a)));
+    };
+    if constexpr (STEP) {
+      need_k = need(k_new);
+      need_v = need(v_new);
+    }
   };
   bool wrote = false;                            // (uniform) this wavefront has the appended row
-  uint32_t new_ks = 0, new_vs = 0;
+  uint32_t k_code = 0, v_code = 0;               // this lane's EPL codes of it
+  float new_ks = 0.f, new_vs = 0.f;
 
   // The first wavefront requests the head's `arrivals` when its last tile's rows have landed, to have the word when the tile is done.
   uint64_t seen = 0;
@@ -231,10 +246,10 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
     looked = true;
   };
 
-  // One tile; V has landed when at most v_wait requests are outstanding.  Returns the group-mean logit of slot row_mine and whether this lane
+  // One tile; it has landed when at most v_wait requests are outstanding.  Returns the group-mean logit of slot row_mine and whether this lane
   // stores it.
   // first: no tile of this wavefront has been computed.  may_own: the appended token may join it (only a wavefront's last live tile).
-  auto compute = [&](int tbase, Tile& t, unsigned char* Vb, bool first, auto may_own, auto v_wait, float& x_out, float& ls_old) -> bool {
+  auto compute = [&](int tbase, const Tile& t, unsigned char* Kb, bool first, auto may_own, auto v_wait, float& x_out, float& ls_old) -> bool {
     constexpr int kVWait = decltype(v_wait)::value;
     const int n_live = min(kQBlock, live_end - tbase);
     x_out = ls_old = 0.f;
@@ -242,49 +257,60 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
     float ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, t.scale), 0));
     float vs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, t.scale), 1));
     const bool own = STEP && decltype(may_own)::value && tbase == own_base;   // uniform
-    bool v_moves = false;
-    float v_ratio = 1.f;
+    unsigned char* const Vb = Kb + TILE_BYTES;
     if (own) {
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kVWait) : "memory");
       wrote = true;
-      const bool k_moves = scale_for(k_new, ks, new_ks);
-      if (k_moves) {
-        const float ratio = ks * inverse_scale(new_ks);
-#pragma unroll
-        for (int st = 0; st < 2; ++st)
-#pragma unroll
-          for (int h = 0; h < KH; ++h) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) t.k[st][h][i] = shift_codes(t.k[st][h][i], ratio);
-            const int r = 16 * st + l16;
-            if (r < new_row) *reinterpret_cast<u32x4_t*>(const_cast<uint8_t*>(kbytes) + (size_t)(tbase + r) * D + 64 * h + 16 * q) = t.k[st][h];
+      // into the tile and, rows moved to a larger scale, back to memory
+      auto join = [&](const float (&x)[EPL], uint32_t need, float& scale, uint32_t& code, unsigned char* rows, uint8_t* memory) {
+        const uint32_t old = __builtin_bit_cast(uint32_t, scale), bits = new_row > 0 ? max(need, old) : need;
+        if (new_row > 0 && bits != old) {        // uniform
+          const float ratio = scale * inverse_scale(bits);
+          for (int i = lane; i < new_row * CHUNKS; i += kWave) {
+            uint4 w = reinterpret_cast<const uint4*>(rows)[i];
+            w = make_uint4(shift_codes(w.x, ratio), shift_codes(w.y, ratio), shift_codes(w.z, ratio), shift_codes(w.w, ratio));
+            reinterpret_cast<uint4*>(rows)[i] = w;
+            const int row = i / CHUNKS, chunk = (i % CHUNKS) ^ swizzle<D>(row);
+            *reinterpret_cast<uint4*>(memory + (size_t)(tbase + row) * D + 16 * chunk) = w;
           }
-      }
-      ks = __builtin_bit_cast(float, new_ks);
-      v_moves = scale_for(v_new, vs, new_vs);
-      v_ratio = vs * inverse_scale(new_vs);
-      vs = __builtin_bit_cast(float, new_vs);
-      encode_row(k_new, new_ks, s_new);
-      encode_row(v_new, new_vs, s_new + D);
+        }
+        scale = __builtin_bit_cast(float, bits);
+        const float inv = inverse_scale(bits);
+        code = encode4(x[0] * inv, EPL == 2 ? x[EPL - 1] * inv : 0.f, 0.f, 0.f);
+        unsigned char* at = rows + new_row * D + ((lane * EPL / 16) ^ swizzle<D>(new_row)) * 16 + lane * EPL % 16;
+        if constexpr (EPL == 2) *reinterpret_cast<uint16_t*>(at) = (uint16_t)code;
+        else *at = (unsigned char)code;
+      };
+      join(k_new, need_k, ks, k_code, Kb, const_cast<uint8_t*>(kbytes));
+      join(v_new, need_v, vs, v_code, Vb, const_cast<uint8_t*>(vbytes));
+      new_ks = ks;
+      new_vs = vs;
       __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
       __builtin_amdgcn_wave_barrier();
-#pragma unroll
-      for (int h = 0; h < KH; ++h) {
-        const u32x4_t w = *reinterpret_cast<const u32x4_t*>(s_new + 64 * h + 16 * q);
-#pragma unroll
-        for (int st = 0; st < 2; ++st) t.k[st][h] = 16 * st + l16 == new_row ? w : t.k[st][h];
-      }
     }
     // ---- S^T = K Q^T
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kVWait + VLOADS) : "memory");      // the K rows
+    u32x4_t kr[2 * KH];                          // [st][h]
+    {
+      const uint32_t at = lds_address(Kb) + (uint32_t)(l16 * D + (q ^ swizzle<D>(l16)) * 16);
+      if constexpr (KH == 2) lds_read4({at, at ^ 64, (at ^ 64) + 16 * D, at + 16 * D}, kr);   // (bit 4 of a row turns bit 2 of its swizzle)
+      else lds_read2(at, (at ^ 32) + 16 * D, kr[0], kr[1]);
+    }
+    bf16x8_t ka[2][KS];
+#pragma unroll
+    for (int st = 0; st < 2; ++st)
+#pragma unroll
+      for (int k_step = 0; k_step < KS; ++k_step) {
+        const u32x4_t w = kr[st * KH + (k_step >> 1)];
+        ka[st][k_step] = expand8(w[2 * (k_step & 1)], w[2 * (k_step & 1) + 1], ks);
+      }
     f32x4_t s[2] = {f32x4_t{0.f, 0.f, 0.f, 0.f}, f32x4_t{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
     for (int term = QTERMS - 1; term >= 0; --term)
 #pragma unroll
       for (int k_step = 0; k_step < KS; ++k_step)
 #pragma unroll
-        for (int st = 0; st < 2; ++st) {
-          const u32x4_t w = t.k[st][k_step >> 1];
-          s[st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(expand8(w[2 * (k_step & 1)], w[2 * (k_step & 1) + 1], ks), qb[term][k_step], s[st], 0, 0, 0);
-        }
+        for (int st = 0; st < 2; ++st) s[st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[st][k_step], qb[term][k_step], s[st], 0, 0, 0);
     float sv[NV];
     take_shares<G>(s, r_l, pos0, sv);
     // ---- logits (log2 domain, log2(votes) folded in), group-mean logit for the EMA
@@ -323,21 +349,8 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
     // (tied to the softmax sum, so that the wait is not scheduled ahead of the arithmetic it is meant to hide)
     asm volatile("s_waitcnt vmcnt(%1)" : "+v"(l_run) : "n"(kVWait) : "memory");
     if (kVWait == 0) look();
-    if (n_live < kQBlock || own) {               // uniform
-      if (v_moves) {
-        for (int i = lane; i < new_row * CHUNKS; i += kWave) {
-          uint4* at = reinterpret_cast<uint4*>(Vb) + i;
-          uint4 w = *at;
-          w = make_uint4(shift_codes(w.x, v_ratio), shift_codes(w.y, v_ratio), shift_codes(w.z, v_ratio), shift_codes(w.w, v_ratio));
-          *at = w;
-          const int row = i / CHUNKS, chunk = (i % CHUNKS) ^ swizzle<D>(row);
-          *reinterpret_cast<uint4*>(const_cast<uint8_t*>(vbytes) + (size_t)(tbase + row) * D + 16 * chunk) = w;
-        }
-      }
-      // rows of masked slots are cleared (0 * NaN would be NaN)
+    if (n_live < kQBlock) {                      // uniform: rows of masked slots are cleared (0 * NaN would be NaN)
       for (int i = n_live * CHUNKS + lane; i < kQBlock * CHUNKS; i += kWave) reinterpret_cast<uint4*>(Vb)[i] = make_uint4(0, 0, 0, 0);
-      if (own && lane < CHUNKS)
-        reinterpret_cast<uint4*>(Vb)[new_row * CHUNKS + (lane ^ swizzle<D>(new_row))] = *reinterpret_cast<const uint4*>(s_new + D + 16 * lane);
       __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
       __builtin_amdgcn_wave_barrier();
     }
@@ -348,8 +361,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
     typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
     u32x2_t b[NTILE];
     uint32_t va[NTILE];
-    const uint32_t va0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)Vb +
-                         (uint32_t)(vrow * D + swizzle<D>(vrow) * 16 + (l16 & 1) * 8);
+    const uint32_t va0 = lds_address(Vb) + (uint32_t)(vrow * D + swizzle<D>(vrow) * 16 + (l16 & 1) * 8);
 #pragma unroll
     for (int nt = 0; nt < NTILE; ++nt) va[nt] = va0 ^ (uint32_t)(nt * 16);
     if constexpr (NTILE == 8)
@@ -385,8 +397,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
     return (lo == -INFINITY) ? hi : hi + kLn2 * fast_log2(1.f + fast_exp2((lo - hi) * kLog2e));
   };
 
-  unsigned char* const s_stage = smem_tiles + kWaves * WAVE_BYTES;
-  const bool staged = kTiles == kLoop && STEP && p.per <= kWaves * kStageSlots;
+  const bool staged = kTiles == kLoop && STEP && p.per <= kWaves * quant_stage_slots<T>(D, G);
   constexpr int kTileStep = kWaves * kQBlock;
   constexpr std::true_type kMayOwn{};
   constexpr std::false_type kNotLast{};
@@ -400,6 +411,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
   if constexpr (kTiles == kOne) {
     if (base < lim) {
       request(base, t0, Tb);
+      read_new();
       read_q(kFirst);
       read_len();
       own0 = compute(base, t0, Tb, true, kMayOwn, kAll, x0, ls0);
@@ -407,11 +419,12 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
   } else if constexpr (kTiles == kTwo) {
     if (base < lim) {
       request(base, t0, Tb);
-      request(base + kTileStep, t1, Tb + TILE_BYTES);                 // (beyond the last row its rows are the last row's)
+      request(base + kTileStep, t1, Tb + BUFFER);                 // (beyond the last row its rows are the last row's)
+      read_new();
       read_q(kBoth);
       read_len();
       own0 = compute(base, t0, Tb, true, kMayOwn, kFirst, x0, ls0);
-      if (base + kTileStep < live_end) own1 = compute(base + kTileStep, t1, Tb + TILE_BYTES, false, kMayOwn, kAll, x1, ls1);
+      if (base + kTileStep < live_end) own1 = compute(base + kTileStep, t1, Tb + BUFFER, false, kMayOwn, kAll, x1, ls1);
     }
   } else {
     auto publish = [&](int tbase, bool mine, float x, float ls_old) {
@@ -420,7 +433,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
         const float r = ema(ls_old, x);
         if (mine) {
           if (staged) {
-            const uint32_t sa = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)(s_stage + (size_t)(tbase - start + row_mine) * 4);
+            const uint32_t sa = lds_address(s_q) + (uint32_t)(((tbase - start) / kTileStep * kQBlock + row_mine) * 4);
             asm volatile("ds_write_b32 %0, %1" : : "v"(sa), "v"(r) : "memory");
           } else {
             p.log_s[ubase + tbase + row_mine] = r;
@@ -433,12 +446,13 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
     // round trip before the wavefront may deposit (40 heads of D 64 x 2892 slots in splits of three tiles 11.0 us with, 8.9 without).
     if (base < lim) {
       request(base, t0, Tb);
-      request(base + kTileStep, t1, Tb + TILE_BYTES);                 // (beyond the last row its rows are the last row's)
+      request(base + kTileStep, t1, Tb + BUFFER);                 // (beyond the last row its rows are the last row's)
+      read_new();
       read_q(kBoth);
       read_len();
-      auto tile = [&](int tb, Tile& t, unsigned char* Vb, auto may_own, auto v_wait) {
+      auto tile = [&](int tb, const Tile& t, unsigned char* buf, auto may_own, auto v_wait) {
         float x, ls;
-        const bool mine = compute(tb, t, Vb, tb == base, may_own, v_wait, x, ls);
+        const bool mine = compute(tb, t, buf, tb == base, may_own, v_wait, x, ls);
         publish(tb, mine, x, ls);
         __builtin_amdgcn_sched_barrier(0);
       };
@@ -447,18 +461,18 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
         tile(tb, t0, Tb, kNotLast, kFirst);
         request(tb + 2 * kTileStep, t0, Tb);
         if (left == 3) {
-          tile(tb + kTileStep, t1, Tb + TILE_BYTES, kNotLast, kFirst);
+          tile(tb + kTileStep, t1, Tb + BUFFER, kNotLast, kFirst);
           tile(tb + 2 * kTileStep, t0, Tb, kMayOwn, kAll);
           left = 0;
           break;
         }
-        tile(tb + kTileStep, t1, Tb + TILE_BYTES, kNotLast, kFirst);
-        request(tb + 3 * kTileStep, t1, Tb + TILE_BYTES);
+        tile(tb + kTileStep, t1, Tb + BUFFER, kNotLast, kFirst);
+        request(tb + 3 * kTileStep, t1, Tb + BUFFER);
         tb += 2 * kTileStep;
         left -= 2;
       }
       if (left > 0) tile(tb, t0, Tb, kMayOwn, kFirst);
-      if (left > 1) tile(tb + kTileStep, t1, Tb + TILE_BYTES, kMayOwn, kAll);
+      if (left > 1) tile(tb + kTileStep, t1, Tb + BUFFER, kMayOwn, kAll);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                  // no copy may land in what follows
   }
@@ -488,21 +502,29 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
     store(base, own0, x0, ls0);
     if constexpr (kTiles == kTwo) store(base + kTileStep, own1, x1, ls1);
   } else if constexpr (STEP) {
+    auto new_score = [&](int j) {                // of the split's slot j: where its tile's wavefront has left it
+      const int tile = j / kQBlock;
+      const unsigned char* of = smem_tiles + (tile % kWaves) * WAVE_BYTES + kBuffers * BUFFER;
+      return reinterpret_cast<const float*>(of)[tile / kWaves * kQBlock + j % kQBlock];
+    };
     if (staged)
       for (int j = threadIdx.x; j < live_end - start; j += kWaves * kWave)
-        __hip_atomic_store(&p.log_s[ubase + start + j], *reinterpret_cast<const float*>(s_stage + (size_t)j * 4), __ATOMIC_RELAXED,
-                           __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(&p.log_s[ubase + start + j], new_score(j), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   if (STEP && wrote) {                           // the appended token joins the cache
-    if (lane < 2 * CHUNKS) {
-      uint8_t* dst = const_cast<uint8_t*>(lane < CHUNKS ? kbytes : vbytes) + (size_t)len_old * D;
-      reinterpret_cast<uint4*>(dst)[lane % CHUNKS] = *reinterpret_cast<const uint4*>(s_new + lane * 16);
+    const size_t at = (size_t)len_old * D + lane * EPL;
+    if constexpr (EPL == 2) {
+      *reinterpret_cast<uint16_t*>(const_cast<uint8_t*>(kbytes) + at) = (uint16_t)k_code;
+      *reinterpret_cast<uint16_t*>(const_cast<uint8_t*>(vbytes) + at) = (uint16_t)v_code;
+    } else {
+      const_cast<uint8_t*>(kbytes)[at] = (uint8_t)k_code;
+      const_cast<uint8_t*>(vbytes)[at] = (uint8_t)v_code;
     }
     if (lane == 0) {
       p.votes[ubase + len_old] = 1;
       p.born[ubase + len_old] = t_word;
-      qp.k_scale[(size_t)unit * blocks + len_old / kQBlock] = __builtin_bit_cast(float, new_ks);
-      qp.v_scale[(size_t)unit * blocks + len_old / kQBlock] = __builtin_bit_cast(float, new_vs);
+      qp.k_scale[(size_t)unit * blocks + len_old / kQBlock] = new_ks;
+      qp.v_scale[(size_t)unit * blocks + len_old / kQBlock] = new_vs;
     }
   }
   combine_and_finish<T, D, G, kWaves, STEP, kWaves, true, kMeet == kSoloMeet, kMayShareXcd>(p, s_ml, s_ml + G, s_acc, kPartStride, kPartStride, &s_last,
@@ -514,7 +536,8 @@ template <typename T, int D, int G>
 keepkv_status launch_quant_g(const QuantParams& p, int units, bool step, hipStream_t st) {
   auto go = [&](auto step_tag, auto tiles_tag, auto meet_tag, auto waves_tag) -> keepkv_status {
     constexpr int kTiles = decltype(tiles_tag)::value, kWaves = decltype(waves_tag)::value;
-    constexpr size_t lds = (size_t)kWaves * (quant_wave_bytes<T>(D, G, kTiles == kOne ? 1 : 2) + (kTiles == kLoop ? kStageSlots * 4 : 0));
+    constexpr size_t lds = (size_t)kWaves * quant_wave_bytes<T>(D, G, kTiles == kOne ? 1 : 2);
+    static_assert(lds + 1024 <= 160 * 1024, "LDS of a compute unit");
     auto* kernel = decode_quant_kernel<T, D, G, decltype(step_tag)::value, kTiles, decltype(meet_tag)::value, kWaves>;
     if constexpr (lds > 60 * 1024) {
       static const bool allowed = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) == hipSuccess;
@@ -526,7 +549,8 @@ keepkv_status launch_quant_g(const QuantParams& p, int units, bool step, hipStre
     return launch_status();
   };
   auto by_waves = [&](auto step_tag, auto tiles_tag, auto meet_tag) {
-    if (p.d.waves == 8) return go(step_tag, tiles_tag, meet_tag, std::integral_constant<int, 8>{});
+    if constexpr (sizeof(T) == 2)                // (f32 layouts have four wavefronts, their queries take twice the room)
+      if (p.d.waves == 8) return go(step_tag, tiles_tag, meet_tag, std::integral_constant<int, 8>{});
     return go(step_tag, tiles_tag, meet_tag, std::integral_constant<int, 4>{});
   };
   auto by_meet = [&](auto step_tag, auto tiles_tag) {
