@@ -1,4 +1,6 @@
 // keepkv_decode_attn_quant / keepkv_decode_step_quant: plans, arguments, entry points.  The kernel is in decode_quant.hpp.
+#include <math.h>
+
 #include "quant_launch.hpp"
 
 namespace kk {
@@ -7,7 +9,21 @@ namespace {
 constexpr int kMaxQuantWorkgroups = 512;         // that share heads: bounds the workspace
 constexpr int kMinQuantSplit = 64;
 
-// Slots per split and workgroup size: the cost model of the bf16 kernel (choose_split in decode_attn.hip) with this kernel's rates.
+// Workgroups that a compute unit holds: by LDS (K and V tiles of one or two buffers and the query rows, per wavefront) and registers.
+int resident_quant(const keepkv_layout* L, long tiles_per_wave, int waves) {
+  const int group = L->n_q_heads / L->n_kv_heads, element = L->dtype == KEEPKV_F32 ? 4 : 2;
+  const int wave = (tiles_per_wave == 1 ? 2 : 4) * kQBlock * L->head_dim + (group * L->head_dim * element + 1023) / 1024 * 1024;
+  const int by_lds = 160 * 1024 / (waves * wave + 1024), by_regs = (tiles_per_wave == 1 ? 24 : 12) / waves;
+  const int n = by_lds < by_regs ? by_lds : by_regs;
+  return n > 0 ? n : 1;
+}
+
+// Slots per split and workgroup size from the kind of cost model that the bf16 kernel has (choose_split in decode_attn.hip): a round of workgroups
+// takes the longer of one workgroup's rows (a compute unit pulls 35 GB/s, shared by its workgroups; a wavefront 8.4 GB/s with all its tiles
+// requested at once, 4.5 in the tile loop) and of all rows (5.7 TB/s, less where compute units stay empty); more rounds, smaller workgroups, a
+// second tile, the loop and combining splits cost what stands below, in us.  The constants are a fit to 6000 measured (shape, plan) pairs of 325
+// shapes (1 to 1024 heads, 64 to 32768 slots, head dims 64 and 128, groups of 1 to 8), of which the plan chosen is 1.6 % slower than the best
+// one (20 % at most); the bf16 kernel's constants 2.3 % (35 %).
 void choose_split_quant(const keepkv_layout* L, int capacity, long& per, int& waves) {
   const double units = (double)L->batch * L->n_kv_heads;
   const int group = L->n_q_heads / L->n_kv_heads;
@@ -15,29 +31,29 @@ void choose_split_quant(const keepkv_layout* L, int capacity, long& per, int& wa
   const long max_ns = (capacity + kMinQuantSplit - 1) / kMinQuantSplit;
   double best = 1e300;
   for (int wv = 4; wv <= (L->dtype == KEEPKV_F32 ? 4 : 8); wv += 4) {
-    const double res_max = 256.0 * (8 / wv);
     for (long ns = 1; ns <= max_ns && (ns == 1 || units * (double)ns <= kMaxQuantWorkgroups); ++ns) {
       long cand = ((capacity + ns - 1) / ns + kQBlock - 1) / kQBlock * kQBlock;
       if (cand < kMinQuantSplit) cand = kMinQuantSplit;
       const double n_split = (double)((capacity + cand - 1) / cand);
       const double wgs = units * n_split;
-      const long tiles = cand / kQBlock;
-      const double busy = (double)(tiles < wv ? tiles : wv);
-      const double streams = (tiles <= 2 * wv ? 8.0 : 6.0) * busy;                    // GB/s
-      auto round_of = [&](double n) {                                                  // us
+      const long tiles = cand / kQBlock, per_wave = (tiles + wv - 1) / wv;
+      const double res_max = 256.0 * resident_quant(L, per_wave, wv);
+      const double streams = (per_wave <= 2 ? 8.4 : 4.5) * (double)(tiles < wv ? tiles : wv);   // GB/s
+      auto round_of = [&](double n) {
         if (n <= 0.0) return 0.0;
         const double per_cu = (double)(long)((n + 255.0) / 256.0);
-        const double rate = 33.7 / per_cu < streams ? 33.7 / per_cu : streams;
+        const double rate = 35.0 / per_cu < streams ? 35.0 / per_cu : streams;
         const double alone = (double)cand * slot_bytes / (rate * 1e3);
-        const double together = n * (units * capacity / wgs) * slot_bytes / (5.8e6 * pow(n / (256.0 * per_cu), 0.38));
+        const double together = n * (units * capacity / wgs) * slot_bytes / (5.7e6 * pow(n / (256.0 * per_cu), 0.30));
         return alone > together ? alone : together;
       };
       const double full = (double)(long)(wgs / res_max), rest = wgs - full * res_max;
       const double rounds = full + (rest > 0.0 ? 1.0 : 0.0);
-      const double elements = (double)((group * L->head_dim + wv * kWave - 1) / (wv * kWave));
-      double t = full * round_of(res_max) + round_of(rest) + 1.7 * (rounds - 1.0) + (wv == 4 ? 0.46 : 0.0);
+      const double elements = (double)((group * L->head_dim + wv * kWave - 1) / (wv * kWave));   // per thread
+      double t = full * round_of(res_max) + round_of(rest) + 4.3 * (rounds - 1.0) + (wv == 4 ? 0.78 : 0.0) +
+                 (per_wave > 2 ? 0.86 : per_wave == 2 ? 0.47 : 0.0);
       if (n_split > 1.0)
-        t += (n_split <= 4.0 ? 1.85 : n_split <= 8.0 ? 2.7 : 4.3 + 1.3 * elements * (double)(long)((n_split - 1.0) / 16.0)) + 0.011 * n_split;
+        t += (n_split <= 4.0 ? 2.15 : n_split <= 8.0 ? 2.78 : 4.33 + 2.05 * elements * (double)(long)((n_split - 1.0) / 16.0)) + 0.0046 * n_split;
       if (t < best) {
         best = t;
         per = cand;
