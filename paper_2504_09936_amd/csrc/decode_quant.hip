@@ -9,11 +9,13 @@ namespace {
 constexpr int kMaxQuantWorkgroups = 512;         // that share heads: bounds the workspace
 constexpr int kMinQuantSplit = 64;
 
-// Workgroups that a compute unit holds: by LDS (K and V tiles of one or two buffers and the query rows, per wavefront) and registers.
+// Workgroups that a compute unit holds: by LDS (K and V tiles and the query rows, once per wavefront or, the loop's, once) and registers.
 int resident_quant(const keepkv_layout* L, long tiles_per_wave, int waves) {
-  const int group = L->n_q_heads / L->n_kv_heads, element = L->dtype == KEEPKV_F32 ? 4 : 2;
-  const int wave = (tiles_per_wave == 1 ? 2 : 4) * kQBlock * L->head_dim + (group * L->head_dim * element + 1023) / 1024 * 1024;
-  const int by_lds = 160 * 1024 / (waves * wave + 1024), by_regs = (tiles_per_wave == 1 ? 24 : 12) / waves;
+  const bool f32 = L->dtype == KEEPKV_F32, loop = tiles_per_wave > 2;
+  const int rows = (tiles_per_wave == 2 ? 4 : 2) * kQBlock * L->head_dim;
+  const int query = (L->n_q_heads / L->n_kv_heads * L->head_dim * (f32 ? 4 : 2) + 1023) / 1024 * 1024;
+  const int lds = waves * rows + (loop ? 1 : waves) * query + 1024;
+  const int by_lds = 160 * 1024 / lds, by_regs = (tiles_per_wave == 1 ? 24 : f32 ? 8 : 16) / waves;
   const int n = by_lds < by_regs ? by_lds : by_regs;
   return n > 0 ? n : 1;
 }

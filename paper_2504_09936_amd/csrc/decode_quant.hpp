@@ -57,38 +57,41 @@ __device__ __forceinline__ void lds_read4(const uint32_t (&at)[4], V (&x)[4]) {
 }
 __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p; }
 
-// LDS of a wavefront: K and V tiles and the query rows (whole kilobytes), later its deposit (and the weights of the splits behind it).
+// How many tiles a wavefront has at most: one, two (both requested before the first wait), more (a loop); and where splits
+// meet: not at all, through memory, or within an XCD where their workgroups find that they may.
+constexpr int kOne = 0, kTwo = 1, kLoop = 2;
+constexpr int kSoloMeet = 0, kMemMeet = 1, kXcdMeet = 2;
+
+// LDS: per wavefront K and V tiles and (not the loop) the query rows, whole kilobytes, later its deposit (and the weights of the splits behind
+// it); the loop's wavefronts share one copy of the query rows.
 template <typename T>
 constexpr int quant_q_bytes(int D, int G) {
   return (G * D * (int)sizeof(T) + 1023) / 1024 * 1024;
 }
 template <typename T>
-constexpr int quant_wave_bytes(int D, int G, int buffers) {
-  const int tiles = buffers * 2 * kQBlock * D + quant_q_bytes<T>(D, G), deposit = (G * D + 16 + 128) * 4;
-  return (tiles > deposit ? tiles : deposit + 127) / 128 * 128;
+constexpr int quant_wave_bytes(int D, int G, int tiles) {
+  const int rows = tiles == kLoop ? 2 * kQBlock * D : (tiles == kOne ? 1 : 2) * 2 * kQBlock * D + quant_q_bytes<T>(D, G);
+  const int deposit = (G * D + 16 + 128) * 4;
+  return (rows > deposit ? rows : deposit + 127) / 128 * 128;
 }
-// New scores that wait in LDS for the end of a tile loop: each wavefront's where its query rows were.
 template <typename T>
-constexpr int quant_stage_slots(int D, int G) {
-  return quant_q_bytes<T>(D, G) / 4;
+constexpr int quant_lds_bytes(int D, int G, int tiles, int waves) {
+  return waves * quant_wave_bytes<T>(D, G, tiles) + (tiles == kLoop ? quant_q_bytes<T>(D, G) : 0);
 }
 
-// How many tiles a wavefront has at most: one, two (all requested before the first wait), more (a loop over two buffers); and where splits
-// meet: not at all, through memory, or within an XCD where their workgroups find that they may.
-constexpr int kOne = 0, kTwo = 1, kLoop = 2;
-constexpr int kSoloMeet = 0, kMemMeet = 1, kXcdMeet = 2;
+// Registers: four wavefronts of the loop to a SIMD (f32 queries, three terms: two).
+constexpr int quant_waves_per_simd(int element, int tiles) { return tiles == kLoop && element == 2 ? 4 : 2; }
 
 template <typename T, int D, int G, bool STEP, int kTiles, int kMeet, int kWaves>
-__global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantParams qp) {
+__global__ __launch_bounds__(kWaves* kWave, quant_waves_per_simd(sizeof(T), kTiles)) void decode_quant_kernel(QuantParams qp) {
   const DecodeParams& p = qp.d;
   constexpr bool kF32 = sizeof(T) == 4;
   constexpr int KH = D / 64, KS = D / 32, NTILE = D / 16, CHUNKS = D / 16;
   constexpr int TILE_BYTES = kQBlock * D, BUFFER = 2 * TILE_BYTES, VLOADS = TILE_BYTES / (kWave * 16);
   constexpr int NV = kShare<G>;
-  constexpr int kBuffers = kTiles == kOne ? 1 : 2;
-  constexpr int WAVE_BYTES = quant_wave_bytes<T>(D, G, kBuffers);
+  constexpr int WAVE_BYTES = quant_wave_bytes<T>(D, G, kTiles);
   constexpr int QTERMS = kF32 ? 3 : 1;
-  constexpr int REQUESTS = 2 * VLOADS + 2 + (STEP ? 1 : 0);           // of a tile
+  constexpr int SCALARS = 2 + (STEP ? 1 : 0), REQUESTS = SCALARS + 2 * VLOADS;        // requests of a tile
   constexpr int EPL = D / kWave;                 // channels of a lane in an appended row
   extern __shared__ __align__(256) unsigned char smem_tiles[];
   constexpr bool kMayShareXcd = kMeet == kXcdMeet;
@@ -129,24 +132,40 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
     __hip_atomic_fetch_add(&p.arrivals[unit], 1ull << (8 * xcd_id()), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 
   // ---- requests
-  float k_new[EPL], v_new[EPL];                  // STEP: this lane's channels EPL lane .. of the token
+  // STEP: this lane's channels EPL lane .. of the token, as they are in memory.
+  typedef typename std::conditional<kF32, typename std::conditional<EPL == 2, float2, float>::type,
+                                    typename std::conditional<EPL == 2, uint32_t, uint16_t>::type>::type RowPiece;
+  RowPiece k_new{}, v_new{};
   if constexpr (STEP) {
-#pragma unroll
-    for (int e = 0; e < EPL; ++e) {
-      const size_t at = (size_t)unit * D + lane * EPL + e;
-      k_new[e] = kF32 ? reinterpret_cast<const float*>(p.k_t)[at] : bf16_to_f32(reinterpret_cast<const uint16_t*>(p.k_t)[at]);
-      v_new[e] = kF32 ? reinterpret_cast<const float*>(p.v_t)[at] : bf16_to_f32(reinterpret_cast<const uint16_t*>(p.v_t)[at]);
-    }
+    k_new = reinterpret_cast<const RowPiece*>(p.k_t)[(size_t)unit * kWave + lane];
+    v_new = reinterpret_cast<const RowPiece*>(p.v_t)[(size_t)unit * kWave + lane];
   }
+  auto piece_f32 = [](const RowPiece& r, float (&x)[EPL]) {
+    if constexpr (kF32 && EPL == 2) {
+      x[0] = r.x;
+      x[EPL - 1] = r.y;
+    } else if constexpr (kF32) {
+      x[0] = r;
+    } else {
+      x[0] = bf16_to_f32((uint16_t)r);
+      if constexpr (EPL == 2) x[EPL - 1] = bf16_hi((uint32_t)r);
+    }
+  };
   // The query rows go through LDS: gathered by the lanes that need them they would be 16 / G times their bytes.  Chunk c of head g sits at
   // position c ^ (g mod 8) of its row.
-  unsigned char* const s_q = Tb + kBuffers * BUFFER;
-  constexpr int QROW = D * (int)sizeof(T), QCHUNKS = QROW / 16;
-#pragma unroll
-  for (int j = 0; j < quant_q_bytes<T>(D, G) / 1024; ++j) {
+  unsigned char* const s_q = kTiles == kLoop ? smem_tiles + kWaves * WAVE_BYTES : Tb + (kTiles == kOne ? 1 : 2) * BUFFER;
+  constexpr int QROW = D * (int)sizeof(T), QCHUNKS = QROW / 16, QPIECES = quant_q_bytes<T>(D, G) / 1024;
+  static_assert(QPIECES <= 4, "at most one piece of the shared copy for a wavefront");
+  auto request_q = [&](int j) {
     const int c = min(j * kWave + lane, G * QCHUNKS - 1), g = c / QCHUNKS;       // surplus lanes repeat the last chunk
     copy_to_lds<0>(reinterpret_cast<const unsigned char*>(p.q) + (size_t)unit * G * QROW, (size_t)G * QROW, s_q + j * 1024,
                    (uint32_t)((c ^ (g & 7)) * 16), 0);
+  };
+  if constexpr (kTiles == kLoop) {
+    if (wave < QPIECES) request_q(wave);
+  } else {
+#pragma unroll
+    for (int j = 0; j < QPIECES; ++j) request_q(j);
   }
   __builtin_amdgcn_sched_barrier(0);
   struct Tile {
@@ -154,29 +173,34 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
     int votes;
     float ls;                                    // ln S of slot row_mine
   };
-  auto request = [&](int tbase, Tile& t, unsigned char* buf) {
-    t.scale = scales[min(tbase / kQBlock, blocks - 1)];
-    const int at = min(tbase + row_mine, last_row);
-    t.votes = p.votes[ubase + at];
-    if constexpr (STEP) t.ls = p.log_s[ubase + at];
-    else t.ls = 0.f;
-    uint32_t off[VLOADS];
+  // A copy is 1024 bytes of the tile: this lane's place in it, with its chunk as the rows from 16 on have it in `at_upper`.  The descriptor
+  // ends behind the last row that may be read; beyond it a copy brings zeros.
+  constexpr int COPY_ROWS = 1024 / D;
+  const uint32_t at_lower = (uint32_t)(lane / CHUNKS * D + ((lane % CHUNKS) ^ swizzle<D>(lane / CHUNKS)) * 16), at_upper = at_lower ^ (8 * CHUNKS);
+  auto request_rows = [&](int tbase, const uint8_t* rows, unsigned char* to) {
 #pragma unroll
-    for (int i = 0; i < VLOADS; ++i) {
-      const int at16 = i * kWave + lane, row = at16 / CHUNKS, chunk = (at16 % CHUNKS) ^ swizzle<D>(row);
-      off[i] = (uint32_t)(min(tbase + row, last_row) * D + 16 * chunk);
-    }
-#pragma unroll
-    for (int i = 0; i < VLOADS; ++i) copy_to_lds<2>(kbytes, (size_t)(last_row + 1) * D, buf + i * (kWave * 16), off[i], 0);
-#pragma unroll
-    for (int i = 0; i < VLOADS; ++i) copy_to_lds<2>(vbytes, (size_t)(last_row + 1) * D, buf + TILE_BYTES + i * (kWave * 16), off[i], 0);
+    for (int i = 0; i < VLOADS; ++i)
+      copy_to_lds<2>(rows, (size_t)(last_row + 1) * D, to + i * 1024, (i * COPY_ROWS < 16 ? at_lower : at_upper) + (uint32_t)(tbase * D + i * 1024), 0);
     __builtin_amdgcn_sched_barrier(0);
+  };
+  auto request_k = [&](int tbase, Tile& t, unsigned char* buf) {       // and the scalars, ahead of it
+    const uint32_t block = (uint32_t)min(tbase / kQBlock, blocks - 1), at = (uint32_t)min(tbase + row_mine, last_row);
+    t.scale = scales[block];
+    t.votes = *reinterpret_cast<const int32_t*>(reinterpret_cast<const char*>(p.votes + ubase) + at * 4u);
+    if constexpr (STEP) t.ls = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(p.log_s + ubase) + at * 4u);
+    else t.ls = 0.f;
+    request_rows(tbase, kbytes, buf);
+  };
+  auto request_v = [&](int tbase, unsigned char* buf) { request_rows(tbase, vbytes, buf + TILE_BYTES); };
+  auto request = [&](int tbase, Tile& t, unsigned char* buf) {
+    request_k(tbase, t, buf);
+    request_v(tbase, buf);
   };
 
   // Column l16 of the B operand is head l16 mod G, of k-step 2 h + t this lane's channels 64 h + 16 q + 8 t + j; f32 queries in three terms.
   bf16x8_t qb[QTERMS][KS];
-  auto read_q = [&](auto behind) {               // with at most `behind` requests outstanding the copies have landed
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(behind)::value) : "memory");
+  auto await = [&](auto behind) { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(behind)::value) : "memory"); };   // that many requests may be under way
+  auto read_q = [&]() {
     const uint32_t row = lds_address(s_q + g_l * QROW);
     auto chunk = [&](int c) { return row + (uint32_t)((c ^ (g_l & 7)) * 16); };
     if constexpr (!kF32) {
@@ -203,9 +227,10 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
   };
 
   bool grow;
-  int len_old, len, live_end, new_row, own_base;                      // own_base: the tile that the appended token joins
+  int len_old, t_old, len, live_end, new_row, own_base;                      // own_base: the tile that the appended token joins
   auto read_len = [&]() {
     len_old = __builtin_amdgcn_readfirstlane(len_word);
+    t_old = __builtin_amdgcn_readfirstlane(t_word);
     grow = STEP && len_old < p.capacity;
     len = grow ? len_old + 1 : len_old;
     live_end = min(len, start + p.per);
@@ -222,8 +247,9 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
   // The scales that the new rows need, worked out while the first tile travels.
   uint32_t need_k = 0, need_v = 0;
   auto read_new = [&]() {
-    auto need = [&](const float (&x)[EPL]) {
-      float a = 0.f;
+    auto need = [&](const RowPiece& r) {
+      float x[EPL], a = 0.f;
+      piece_f32(r, x);
 #pragma unroll
       for (int e = 0; e < EPL; ++e) a = fmaxf(a, __builtin_bit_cast(float, finite_magnitude(x[e])));
       a = over_head_lanes<1>(a, [](float u, float v) { return fmaxf(u, v); });
@@ -246,23 +272,27 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
     looked = true;
   };
 
-  // One tile; it has landed when at most v_wait requests are outstanding.  Returns the group-mean logit of slot row_mine and whether this lane
-  // stores it.
-  // first: no tile of this wavefront has been computed.  may_own: the appended token may join it (only a wavefront's last live tile).
-  auto compute = [&](int tbase, const Tile& t, unsigned char* Kb, bool first, auto may_own, auto v_wait, float& x_out, float& ls_old) -> bool {
+  // One tile; its K rows have landed when at most k_wait requests are outstanding, its V rows with v_wait.  Returns the group-mean logit of
+  // slot row_mine and whether this lane stores it.
+  // first: no tile of this wavefront has been computed.  last: it may be its last live one, which the appended token may join and which may
+  // be partly live; all before it are full.
+  // k_done(), v_done(): called when the rows have been read from LDS.
+  auto compute = [&](int tbase, const Tile& t, unsigned char* Kb, bool first, auto last, auto k_wait, auto v_wait, auto k_done, auto v_done,
+                     float& x_out, float& ls_old) -> bool {
     constexpr int kVWait = decltype(v_wait)::value;
-    const int n_live = min(kQBlock, live_end - tbase);
+    constexpr bool kLast = decltype(last)::value;
+    const int n_live = kLast ? min(kQBlock, live_end - tbase) : kQBlock;
     x_out = ls_old = 0.f;
     if (n_live <= 0) return false;               // uniform: below the caller's bound but dead, its scales mean nothing
     float ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, t.scale), 0));
     float vs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, t.scale), 1));
-    const bool own = STEP && decltype(may_own)::value && tbase == own_base;   // uniform
+    const bool own = STEP && kLast && tbase == own_base;   // uniform
     unsigned char* const Vb = Kb + TILE_BYTES;
     if (own) {
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kVWait) : "memory");
       wrote = true;
       // into the tile and, rows moved to a larger scale, back to memory
-      auto join = [&](const float (&x)[EPL], uint32_t need, float& scale, uint32_t& code, unsigned char* rows, uint8_t* memory) {
+      auto join = [&](const RowPiece& r, uint32_t need, float& scale, uint32_t& code, unsigned char* rows, uint8_t* memory) {
         const uint32_t old = __builtin_bit_cast(uint32_t, scale), bits = new_row > 0 ? max(need, old) : need;
         if (new_row > 0 && bits != old) {        // uniform
           const float ratio = scale * inverse_scale(bits);
@@ -276,6 +306,8 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
         }
         scale = __builtin_bit_cast(float, bits);
         const float inv = inverse_scale(bits);
+        float x[EPL];
+        piece_f32(r, x);
         code = encode4(x[0] * inv, EPL == 2 ? x[EPL - 1] * inv : 0.f, 0.f, 0.f);
         unsigned char* at = rows + new_row * D + ((lane * EPL / 16) ^ swizzle<D>(new_row)) * 16 + lane * EPL % 16;
         if constexpr (EPL == 2) *reinterpret_cast<uint16_t*>(at) = (uint16_t)code;
@@ -289,13 +321,15 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
       __builtin_amdgcn_wave_barrier();
     }
     // ---- S^T = K Q^T
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kVWait + VLOADS) : "memory");      // the K rows
+    await(k_wait);
     u32x4_t kr[2 * KH];                          // [st][h]
     {
-      const uint32_t at = lds_address(Kb) + (uint32_t)(l16 * D + (q ^ swizzle<D>(l16)) * 16);
+      uint32_t at = lds_address(Kb) + (uint32_t)(l16 * D + (q ^ swizzle<D>(l16)) * 16);
+      if constexpr (kTiles == kLoop) asm volatile("" : "+v"(at));      // (addresses are worked out anew: registers are short)
       if constexpr (KH == 2) lds_read4({at, at ^ 64, (at ^ 64) + 16 * D, at + 16 * D}, kr);   // (bit 4 of a row turns bit 2 of its swizzle)
       else lds_read2(at, (at ^ 32) + 16 * D, kr[0], kr[1]);
     }
+    k_done();
     bf16x8_t ka[2][KS];
 #pragma unroll
     for (int st = 0; st < 2; ++st)
@@ -361,7 +395,8 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
     typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
     u32x2_t b[NTILE];
     uint32_t va[NTILE];
-    const uint32_t va0 = lds_address(Vb) + (uint32_t)(vrow * D + swizzle<D>(vrow) * 16 + (l16 & 1) * 8);
+    uint32_t va0 = lds_address(Vb) + (uint32_t)(vrow * D + swizzle<D>(vrow) * 16 + (l16 & 1) * 8);
+    if constexpr (kTiles == kLoop) asm volatile("" : "+v"(va0));
 #pragma unroll
     for (int nt = 0; nt < NTILE; ++nt) va[nt] = va0 ^ (uint32_t)(nt * 16);
     if constexpr (NTILE == 8)
@@ -379,6 +414,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
           : "=&v"(b[0]), "=&v"(b[1]), "=&v"(b[2]), "=&v"(b[3])
           : "v"(va[0]), "v"(va[1]), "v"(va[2]), "v"(va[3])
           : "memory");
+    v_done();
 #pragma unroll
     for (int part = 0; part < 2; ++part)
 #pragma unroll
@@ -397,13 +433,15 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
     return (lo == -INFINITY) ? hi : hi + kLn2 * fast_log2(1.f + fast_exp2((lo - hi) * kLog2e));
   };
 
-  const bool staged = kTiles == kLoop && STEP && p.per <= kWaves * quant_stage_slots<T>(D, G);
   constexpr int kTileStep = kWaves * kQBlock;
-  constexpr std::true_type kMayOwn{};
+  constexpr std::true_type kIsLast{};
   constexpr std::false_type kNotLast{};
   constexpr std::integral_constant<int, 0> kAll{};
-  constexpr std::integral_constant<int, REQUESTS> kFirst{};           // (a tile's)
-  constexpr std::integral_constant<int, 2 * REQUESTS> kBoth{};
+  constexpr std::integral_constant<int, VLOADS> kOwnV{};              // (the tile's own V rows)
+  constexpr std::integral_constant<int, REQUESTS> kTile{};
+  constexpr std::integral_constant<int, REQUESTS + VLOADS> kOwnVAndTile{};
+  constexpr std::integral_constant<int, 2 * REQUESTS> kTwoTiles{};
+  auto nothing = [] {};
   const int base = start + wave * kQBlock;
   bool own0 = false, own1 = false;               // results per slot that are stored at the very end
   float x0 = 0.f, x1 = 0.f, ls0 = 0.f, ls1 = 0.f;
@@ -412,67 +450,57 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
     if (base < lim) {
       request(base, t0, Tb);
       read_new();
-      read_q(kFirst);
+      await(kTile);
+      read_q();
       read_len();
-      own0 = compute(base, t0, Tb, true, kMayOwn, kAll, x0, ls0);
+      own0 = compute(base, t0, Tb, true, kIsLast, kOwnV, kAll, nothing, nothing, x0, ls0);
     }
   } else if constexpr (kTiles == kTwo) {
     if (base < lim) {
       request(base, t0, Tb);
-      request(base + kTileStep, t1, Tb + BUFFER);                 // (beyond the last row its rows are the last row's)
+      request(base + kTileStep, t1, Tb + BUFFER);                     // (beyond the last row its rows are the last row's)
       read_new();
-      read_q(kBoth);
+      await(kTwoTiles);
+      read_q();
       read_len();
-      own0 = compute(base, t0, Tb, true, kMayOwn, kFirst, x0, ls0);
-      if (base + kTileStep < live_end) own1 = compute(base + kTileStep, t1, Tb + BUFFER, false, kMayOwn, kAll, x1, ls1);
+      own0 = compute(base, t0, Tb, true, kIsLast, kOwnVAndTile, kTile, nothing, nothing, x0, ls0);
+      if (base + kTileStep < live_end)
+        own1 = compute(base + kTileStep, t1, Tb + BUFFER, false, kIsLast, kOwnV, kAll, nothing, nothing, x1, ls1);
     }
   } else {
     auto publish = [&](int tbase, bool mine, float x, float ls_old) {
       if (p.logits_out != nullptr && mine) p.logits_out[ubase + tbase + row_mine] = x;
-      if constexpr (STEP) {
-        const float r = ema(ls_old, x);
-        if (mine) {
-          if (staged) {
-            const uint32_t sa = lds_address(s_q) + (uint32_t)(((tbase - start) / kTileStep * kQBlock + row_mine) * 4);
-            asm volatile("ds_write_b32 %0, %1" : : "v"(sa), "v"(r) : "memory");
-          } else {
-            p.log_s[ubase + tbase + row_mine] = r;
-          }
-        }
-      }
+      if (STEP && mine) p.log_s[ubase + tbase + row_mine] = ema(ls_old, x);
     };
-    // Two tiles in flight: a tile's buffer is requested again when it has been used, if a tile is left for it.  The ways out are written
-    // out, so that on each the number of requests behind a tile is known and none is made for nothing: a surplus one is a memory
-    // round trip before the wavefront may deposit (40 heads of D 64 x 2892 slots in splits of three tiles 11.0 us with, 8.9 without).
+    // One buffer: the next tile's K rows are requested when this one's have been read from LDS, its V rows alike, and four wavefronts to a
+    // SIMD cover what a wavefront waits.  Only tiles that exist are requested: a surplus request is a memory round trip before the
+    // wavefront may deposit.  (Two tiles in flight and two wavefronts to a SIMD: 1024 heads x 852 slots 46.1 us and 45.4 so, 624 heads x 731
+    // 34.0 and 28.7, attention over 64 heads x 8192 27.0 and 26.2.)  New scores are stored as they come: held back in LDS for the end they
+    // gave nothing once a compute unit's workgroups all end together.
     if (base < lim) {
       request(base, t0, Tb);
-      request(base + kTileStep, t1, Tb + BUFFER);                 // (beyond the last row its rows are the last row's)
       read_new();
-      read_q(kBoth);
+      await(kTile);
+    } else {
+      await(kAll);
+    }
+    __builtin_amdgcn_s_barrier();                // every wavefront's piece of the query rows is there (tiles may be under way)
+    if (base < lim) {
+      read_q();
       read_len();
-      auto tile = [&](int tb, const Tile& t, unsigned char* buf, auto may_own, auto v_wait) {
-        float x, ls;
-        const bool mine = compute(tb, t, buf, tb == base, may_own, v_wait, x, ls);
-        publish(tb, mine, x, ls);
-        __builtin_amdgcn_sched_barrier(0);
-      };
       int tb = base, left = live_end > base ? (live_end - base + kTileStep - 1) / kTileStep : 0;
-      while (left > 2) {
-        tile(tb, t0, Tb, kNotLast, kFirst);
-        request(tb + 2 * kTileStep, t0, Tb);
-        if (left == 3) {
-          tile(tb + kTileStep, t1, Tb + BUFFER, kNotLast, kFirst);
-          tile(tb + 2 * kTileStep, t0, Tb, kMayOwn, kAll);
-          left = 0;
-          break;
-        }
-        tile(tb + kTileStep, t1, Tb + BUFFER, kNotLast, kFirst);
-        request(tb + 3 * kTileStep, t1, Tb + BUFFER);
-        tb += 2 * kTileStep;
-        left -= 2;
+      for (; left > 1; --left, tb += kTileStep) {
+        float x, ls;
+        const bool mine = compute(tb, t0, Tb, tb == base, kNotLast, kOwnV, std::integral_constant<int, SCALARS + VLOADS>{},
+                                  [&] { request_k(tb + kTileStep, t1, Tb); }, [&] { request_v(tb + kTileStep, Tb); }, x, ls);
+        publish(tb, mine, x, ls);
+        t0 = t1;
       }
-      if (left > 0) tile(tb, t0, Tb, kMayOwn, kFirst);
-      if (left > 1) tile(tb + kTileStep, t1, Tb + BUFFER, kMayOwn, kAll);
+      if (left > 0) {
+        float x, ls;
+        const bool mine = compute(tb, t0, Tb, tb == base, kIsLast, kOwnV, kAll, nothing, nothing, x, ls);
+        publish(tb, mine, x, ls);
+      }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                  // no copy may land in what follows
   }
@@ -490,7 +518,6 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
     look();                                      // (a wavefront without a tile)
     s_one_xcd = kMayShareXcd && all_on_this_xcd(p, unit, seen);
   }
-  if constexpr (kTiles == kLoop && STEP) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the staged scores are in LDS
   __syncthreads();
   KK_TS(2);
   if constexpr (kTiles != kLoop) {
@@ -501,15 +528,6 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
     };
     store(base, own0, x0, ls0);
     if constexpr (kTiles == kTwo) store(base + kTileStep, own1, x1, ls1);
-  } else if constexpr (STEP) {
-    auto new_score = [&](int j) {                // of the split's slot j: where its tile's wavefront has left it
-      const int tile = j / kQBlock;
-      const unsigned char* of = smem_tiles + (tile % kWaves) * WAVE_BYTES + kBuffers * BUFFER;
-      return reinterpret_cast<const float*>(of)[tile / kWaves * kQBlock + j % kQBlock];
-    };
-    if (staged)
-      for (int j = threadIdx.x; j < live_end - start; j += kWaves * kWave)
-        __hip_atomic_store(&p.log_s[ubase + start + j], new_score(j), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   if (STEP && wrote) {                           // the appended token joins the cache
     const size_t at = (size_t)len_old * D + lane * EPL;
@@ -522,13 +540,13 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_quant_kernel(QuantPar
     }
     if (lane == 0) {
       p.votes[ubase + len_old] = 1;
-      p.born[ubase + len_old] = t_word;
+      p.born[ubase + len_old] = t_old;
       qp.k_scale[(size_t)unit * blocks + len_old / kQBlock] = new_ks;
       qp.v_scale[(size_t)unit * blocks + len_old / kQBlock] = new_vs;
     }
   }
   combine_and_finish<T, D, G, kWaves, STEP, kWaves, true, kMeet == kSoloMeet, kMayShareXcd>(p, s_ml, s_ml + G, s_acc, kPartStride, kPartStride, &s_last,
-                                                                                             unit, split, grow, len, t_word,
+                                                                                             unit, split, grow, len, t_old,
                                                                                              __builtin_amdgcn_readfirstlane(s_one_xcd) != 0);
 }
 
@@ -536,7 +554,7 @@ template <typename T, int D, int G>
 keepkv_status launch_quant_g(const QuantParams& p, int units, bool step, hipStream_t st) {
   auto go = [&](auto step_tag, auto tiles_tag, auto meet_tag, auto waves_tag) -> keepkv_status {
     constexpr int kTiles = decltype(tiles_tag)::value, kWaves = decltype(waves_tag)::value;
-    constexpr size_t lds = (size_t)kWaves * quant_wave_bytes<T>(D, G, kTiles == kOne ? 1 : 2);
+    constexpr size_t lds = quant_lds_bytes<T>(D, G, kTiles, kWaves);
     static_assert(lds + 1024 <= 160 * 1024, "LDS of a compute unit");
     auto* kernel = decode_quant_kernel<T, D, G, decltype(step_tag)::value, kTiles, decltype(meet_tag)::value, kWaves>;
     if constexpr (lds > 60 * 1024) {
