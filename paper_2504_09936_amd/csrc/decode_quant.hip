@@ -21,11 +21,10 @@ int resident_quant(const keepkv_layout* L, long tiles_per_wave, int waves) {
 }
 
 // Slots per split and workgroup size from the kind of cost model that the bf16 kernel has (choose_split in decode_attn.hip): a round of workgroups
-// takes the longer of one workgroup's rows (a compute unit pulls 35 GB/s, shared by its workgroups; a wavefront 8.4 GB/s with all its tiles
-// requested at once, 4.5 in the tile loop) and of all rows (5.7 TB/s, less where compute units stay empty); more rounds, smaller workgroups, a
-// second tile, the loop and combining splits cost what stands below, in us.  The constants are a fit to 6000 measured (shape, plan) pairs of 325
-// shapes (1 to 1024 heads, 64 to 32768 slots, head dims 64 and 128, groups of 1 to 8), of which the plan chosen is 1.6 % slower than the best
-// one (20 % at most); the bf16 kernel's constants 2.3 % (35 %).
+// takes the longer of one workgroup's rows (a compute unit pulls 36 GB/s, shared by its workgroups; a wavefront 25 GB/s, 19 in the tile loop) and of
+// all rows (6.2 TB/s); more rounds, smaller workgroups, a second tile, the loop and combining splits cost what stands below, in us.  The
+// constants are a fit to 7042 measured (shape, plan) pairs of 375 shapes (1 to 1024 heads, 64 to 32768 slots, head dims 64 and 128, groups of 1 to
+// 8), of which the plan chosen is 1.6 % slower than the best one (20 % at most).
 void choose_split_quant(const keepkv_layout* L, int capacity, long& per, int& waves) {
   const double units = (double)L->batch * L->n_kv_heads;
   const int group = L->n_q_heads / L->n_kv_heads;
@@ -40,22 +39,22 @@ void choose_split_quant(const keepkv_layout* L, int capacity, long& per, int& wa
       const double wgs = units * n_split;
       const long tiles = cand / kQBlock, per_wave = (tiles + wv - 1) / wv;
       const double res_max = 256.0 * resident_quant(L, per_wave, wv);
-      const double streams = (per_wave <= 2 ? 8.4 : 4.5) * (double)(tiles < wv ? tiles : wv);   // GB/s
+      const double streams = (per_wave <= 2 ? 25.0 : 19.0) * (double)(tiles < wv ? tiles : wv);   // GB/s
       auto round_of = [&](double n) {
         if (n <= 0.0) return 0.0;
         const double per_cu = (double)(long)((n + 255.0) / 256.0);
-        const double rate = 35.0 / per_cu < streams ? 35.0 / per_cu : streams;
+        const double rate = 36.0 / per_cu < streams ? 36.0 / per_cu : streams;
         const double alone = (double)cand * slot_bytes / (rate * 1e3);
-        const double together = n * (units * capacity / wgs) * slot_bytes / (5.7e6 * pow(n / (256.0 * per_cu), 0.30));
+        const double together = n * (units * capacity / wgs) * slot_bytes / (6.2e6 * pow(n / (256.0 * per_cu), 0.016));
         return alone > together ? alone : together;
       };
       const double full = (double)(long)(wgs / res_max), rest = wgs - full * res_max;
       const double rounds = full + (rest > 0.0 ? 1.0 : 0.0);
       const double elements = (double)((group * L->head_dim + wv * kWave - 1) / (wv * kWave));   // per thread
-      double t = full * round_of(res_max) + round_of(rest) + 4.3 * (rounds - 1.0) + (wv == 4 ? 0.78 : 0.0) +
-                 (per_wave > 2 ? 0.86 : per_wave == 2 ? 0.47 : 0.0);
+      double t = full * round_of(res_max) + round_of(rest) + 1.9 * (rounds - 1.0) + (wv == 4 ? 2.0 : 0.0) +
+                 (per_wave > 2 ? 0.49 : per_wave == 2 ? 0.67 : 0.0);
       if (n_split > 1.0)
-        t += (n_split <= 4.0 ? 2.15 : n_split <= 8.0 ? 2.78 : 4.33 + 2.05 * elements * (double)(long)((n_split - 1.0) / 16.0)) + 0.0046 * n_split;
+        t += (n_split <= 4.0 ? 2.26 : n_split <= 8.0 ? 2.95 : 3.9 + 3.0 * elements * (double)(long)((n_split - 1.0) / 16.0)) + 0.010 * n_split;
       if (t < best) {
         best = t;
         per = cand;
