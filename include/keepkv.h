@@ -296,7 +296,8 @@ keepkv_status keepkv_prefill_merge(const keepkv_layout *layout, const keepkv_cac
  * a <= 448 * 2^e, -110 <= e <= 120, and a code is the row's element / scale rounded to nearest even; an element that is not
  * finite becomes NaN.  Since a scale is a power of two, dividing by it rounds nothing, reading back is exact (in f32 and in
  * bf16), and rows that were read back are quantised again to the same values except where those become subnormal under a
- * larger scale (a value below 2^-6 of the scale keeps multiples of 2^-9 of it).
+ * larger scale (a value below 2^-6 of the scale keeps multiples of 2^-9 of it).  Numbers within 2^-4 of the largest f32 may
+ * round to 2^128, which reads back as infinity.  Scales are read by their exponent: caches hold what these calls have written.
  * Half the bytes of a bf16 cache, and its decode calls read them as they are. */
 #define KEEPKV_QUANT_BLOCK 32
 
@@ -305,7 +306,7 @@ keepkv_status keepkv_prefill_merge(const keepkv_layout *layout, const keepkv_cac
  * rows of the layout's dtype: give them a cache that keepkv_dequantize has written. */
 typedef struct {
   keepkv_cache c;       /* as described there, but k, v: DEVICE uint8 [B, Hkv, capacity, D] e4m3 codes;  */
-                        /* plan_wavefronts 0, 4 or 8                                                    */
+                        /* plan_wavefronts 0, 4 or 8 (f32 layouts always have 4)                          */
   float *k_scale;       /* [B, Hkv, ceil(capacity / KEEPKV_QUANT_BLOCK)] scale of each block of K codes;  */
   float *v_scale;       /* and of V codes.  Those of blocks without a live slot mean nothing             */
 } keepkv_quant_cache;

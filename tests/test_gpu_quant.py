@@ -318,6 +318,101 @@ def test_step(B, H, G, D, dtype, cap, lens, per, waves):
         assert not ws[:64 * 1024 + 256].any()
 
 
+@pytest.mark.parametrize("G,D,dtype,cap,per,waves", [(4, 128, "bf16", 1000, 0, 0), (1, 64, "bf16", 1000, 128, 4), (8, 128, "bf16", 1000, 256, 4),
+                                                     (2, 128, "f32", 1000, 256, 4), (4, 64, "bf16", 1000, 1024, 8)])
+def test_a_bound_far_above_the_lengths(G, D, dtype, cap, per, waves):
+    """The caller's bound may be any number of slots too high: tiles behind the live ones are dead, their codes and scales NaN."""
+    kk = U.kk()
+    g = gen(61)
+    lay = T.layout(1, 6, G, D, dtype)
+    c = T.state(g, lay, cap, [[0, 1, 31, 64, 500, 999]], 2.0)
+    c.plan_slots_per_split, c.plan_wavefronts = per, waves
+    ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+    kk.workspace_init(ws)
+    q = T.rows(g, (1, 6 * G, D), dtype) * 3
+    for hint in (cap, cap + 5000):
+        c.len_hint = hint
+        out, lse = torch.full_like(q, 7.0), torch.zeros((1, 6 * G), device="cuda")
+        kk.decode_attn_quant(lay, c, q, out, None, lse, ws)
+        check_attention(lay, c, q, out, None, lse)
+        k_t, v_t = T.rows(g, (1, 6, D), dtype, 4.0), T.rows(g, (1, 6, D), dtype, 4.0)
+        before = copy_of(kk, lay, c)
+        kk.decode_step_quant(lay, c, q, k_t, v_t, out, None, ALPHA, None, ws)
+        check_step(lay, c, before, q, k_t, v_t, out, None, f"hint {hint}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_token_that_is_not_finite(D, dtype):
+    """Its codes are NaN where it is not finite, the scale comes from the rest, and its head alone is affected."""
+    kk = U.kk()
+    g = gen(62)
+    lay = T.layout(1, 3, 2, D, dtype)
+    c = T.state(g, lay, 100, [[40, 64, 41]])
+    before = copy_of(kk, lay, c)
+    k_t, v_t = T.rows(g, (1, 3, D), dtype, 4.0), T.rows(g, (1, 3, D), dtype, 4.0)
+    v_t[0, 0, 5], v_t[0, 0, D - 1], v_t[0, 1] = float("inf"), float("nan"), float("-inf")
+    q = T.rows(g, (1, 6, D), dtype)
+    out = torch.zeros_like(q)
+    kk.decode_step_quant(lay, c, q, k_t, v_t, out, None, ALPHA, None, kk.new_workspace(lay, 100, 100))
+    torch.cuda.synchronize()
+    for h in range(3):
+        check_head(c, 0, h, *(Q.append(*x, U.to_host(t)[0, h][None]) for x, t in zip(T.head(before, 0, h), (k_t, v_t))))
+    nan = torch.isnan(out[0]).cpu()
+    want = torch.zeros_like(nan)
+    want[:2, 5] = want[:2, D - 1] = True
+    want[2:4] = True
+    assert torch.equal(nan, want)
+    live = torch.arange(100, device="cuda") < c.len.unsqueeze(-1)
+    assert torch.isfinite(c.log_s[live]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scales_at_the_ends_of_their_range(dtype):
+    """Blocks of the smallest and of very large rows in one head, zeros among them."""
+    kk = U.kk()
+    lay = T.layout(1, 2, 4, 64, dtype)
+    g = gen(63)
+    src, c = kk.Cache(lay, 256), kk.QuantCache(lay, 256)
+    k, v = torch.randn(1, 2, 256, 64, generator=g, device="cuda"), torch.randn(1, 2, 256, 64, generator=g, device="cuda")
+    factor = torch.tensor([2.0 ** e for e in (-120, -100, -60, 0, 30, 90, -126, 0)], device="cuda").repeat_interleave(32)
+    v *= factor[:, None]
+    k *= torch.where(factor > 1, torch.ones_like(factor), factor)[:, None]
+    v[0, 1, 224:] = 0
+    src.k.copy_(k)
+    src.v.copy_(v)
+    src.votes.fill_(1)
+    src.len.fill_(250)
+    kk.quantize(lay, src, c)
+    q = T.rows(g, (1, 8, 64), dtype)
+    out, lse = torch.zeros_like(q), torch.zeros((1, 8), device="cuda")
+    kk.decode_attn_quant(lay, c, q, out, None, lse, kk.new_workspace(lay, 256, 256))
+    check_attention(lay, c, q, out, None, lse)
+    torch.cuda.synchronize()
+    for h in range(2):
+        check_head(c, 0, h, Q.quantize(U.to_host(src.k)[0, h, :250]), Q.quantize(U.to_host(src.v)[0, h, :250]))
+
+
+def test_one_workspace_for_caches_of_many_shapes():
+    """In turn on one stream: every call leaves the control words clear for the next one."""
+    kk = U.kk()
+    g = gen(64)
+    ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+    ws.random_(0, 256, generator=g)
+    kk.workspace_init(ws)
+    for B, H, G, D, dtype, cap in [(2, 8, 4, 128, "bf16", 884), (1, 4, 1, 64, "f32", 700), (1, 8, 8, 64, "bf16", 3000), (5, 3, 2, 128, "bf16", 200),
+                                   (1, 8, 4, 128, "bf16", 884)]:
+        lay = T.layout(B, H, G, D, dtype)
+        assert kk.workspace_bytes(lay, cap, cap) <= ws.numel()
+        c = T.state(g, lay, cap, cap - 9)
+        before = copy_of(kk, lay, c)
+        q, k_t, v_t = T.rows(g, (B, H * G, D), dtype), T.rows(g, (B, H, D), dtype), T.rows(g, (B, H, D), dtype)
+        out = torch.zeros_like(q)
+        kk.decode_step_quant(lay, c, q, k_t, v_t, out, None, ALPHA, None, ws)
+        check_step(lay, c, before, q, k_t, v_t, out, None, str((B, H, G, D)))
+        assert not ws[:64 * 1024 + 256].any()
+
+
 def test_step_equals_its_three_calls():
     kk = U.kk()
     g = gen(11)
