@@ -1,7 +1,5 @@
 // keepkv_quantize, keepkv_dequantize, keepkv_append_quant: rows into e4m3 codes with a power-of-two scale per block of 32 slots,
 // and back.  All three move bytes; the arithmetic is a maximum, a multiplication and a conversion per element.
-#include <type_traits>
-
 #include "quant_common.hpp"
 
 namespace kk {
