@@ -458,7 +458,7 @@ __global__ __launch_bounds__(kWaves* kWave, quant_waves_per_simd(sizeof(T), kTil
   } else if constexpr (kTiles == kTwo) {
     if (base < lim) {
       request(base, t0, Tb);
-      request(base + kTileStep, t1, Tb + BUFFER);                     // (beyond the last row its rows are the last row's)
+      request(base + kTileStep, t1, Tb + BUFFER);                     // (beyond the last row its copies bring zeros)
       read_new();
       await(kTwoTiles);
       read_q();
