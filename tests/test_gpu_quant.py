@@ -393,6 +393,66 @@ def test_scales_at_the_ends_of_their_range(dtype):
         check_head(c, 0, h, Q.quantize(U.to_host(src.k)[0, h, :250]), Q.quantize(U.to_host(src.v)[0, h, :250]))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("per", [0, 64])
+def test_slots_without_votes(per, dtype):
+    """A live slot with no votes has weight zero; a head of nothing but such slots gives what keepkv_decode_attn gives on its rows."""
+    kk = U.kk()
+    g = gen(71)
+    lay = T.layout(1, 3, 4, 128, dtype)
+    c = T.state(g, lay, 300, [[300, 290, 97]], 2.0)
+    c.plan_slots_per_split = per
+    c.votes[0, 0, 5:200] = 0
+    c.votes[0, 1, :290] = 0
+    c.votes[0, 2, 96] = 0
+    q = T.rows(g, (1, 12, 128), dtype) * 3
+    ws = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+    kk.workspace_init(ws)
+    out, lse = torch.full_like(q, 7.0), torch.full((1, 12), 7.0, device="cuda")
+    kk.decode_attn_quant(lay, c, q, out, None, lse, ws)
+    r = kk.Cache(lay, 300)
+    kk.dequantize(lay, c, r)
+    want, want_lse = torch.full_like(q, 7.0), torch.full((1, 12), 7.0, device="cuda")
+    kk.decode_attn(lay, r, q, want, None, want_lse, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(out[0, 4:8], want[0, 4:8]) and torch.equal(lse[0, 4:8], want_lse[0, 4:8])
+    with np.errstate(divide="ignore"):
+        for h in (0, 2):
+            (o, l, _), (eo, el, _) = T.attention(c, lay, q, 0, h)
+            assert (np.abs(U.to_host(out)[0, 4 * h:4 * h + 4] - o) <= eo).all(), h
+            assert (np.abs(lse[0, 4 * h:4 * h + 4].cpu().numpy() - l) <= el).all(), h
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_random_shapes(seed):
+    """Attention and two steps on a shape, lengths, a bound on them and a plan drawn at random."""
+    kk = U.kk()
+    rng, g = np.random.default_rng(seed), gen(1000 + seed)
+    dtype, D, G = str(rng.choice(["bf16", "bf16", "f32"])), int(rng.choice([64, 128])), int(rng.choice([1, 2, 4, 8]))
+    B, H = (int(x) for x in rng.integers(1, [4, 9]))
+    cap = int(2 ** rng.uniform(0, 11.5))
+    lay = T.layout(B, H, G, D, dtype)
+    lens = np.where(rng.random((B, H)) < 0.2, rng.choice([0, 1, cap], (B, H)), rng.integers(0, cap + 1, (B, H)))
+    c = T.state(g, lay, cap, lens, float(rng.choice([1.0, 2.0, 8.0])))
+    if rng.random() < 0.6:
+        c.plan_slots_per_split, c.plan_wavefronts = int(rng.choice([0, 64, 96, 128, 320, 512, 2048])), int(rng.choice([0, 4, 8]))
+    ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+    kk.workspace_init(ws)
+    hints = [0, int(lens.max()) + 1, cap + 3]
+    q = T.rows(g, (B, H * G, D), dtype, 2.0)
+    out, lse, logits = torch.full_like(q, 7.0), torch.full((B, H * G), 7.0, device="cuda"), torch.full((B, H, cap), 7.0, device="cuda")
+    c.len_hint = hints[seed % 3]
+    kk.decode_attn_quant(lay, c, q, out, logits, lse, ws)
+    check_attention(lay, c, q, out, logits, lse, f"seed {seed}")
+    for i in range(2):
+        k_t, v_t = T.rows(g, (B, H, D), dtype, 8.0), T.rows(g, (B, H, D), dtype, 8.0)
+        before = copy_of(kk, lay, c)
+        c.len_hint = hints[(seed + i) % 3]
+        kk.decode_step_quant(lay, c, q, k_t, v_t, out, logits if i else None, ALPHA, None, ws)
+        check_step(lay, c, before, q, k_t, v_t, out, logits if i else None, f"seed {seed} step {i}")
+    assert not ws[:64 * 1024 + 256].any()
+
+
 def test_one_workspace_for_caches_of_many_shapes():
     """In turn on one stream: every call leaves the control words clear for the next one."""
     kk = U.kk()
