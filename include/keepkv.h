@@ -306,7 +306,7 @@ keepkv_status keepkv_prefill_merge(const keepkv_layout *layout, const keepkv_cac
  * rows of the layout's dtype: give them a cache that keepkv_dequantize has written. */
 typedef struct {
   keepkv_cache c;       /* as described there, but k, v: DEVICE uint8 [B, Hkv, capacity, D] e4m3 codes;  */
-                        /* plan_wavefronts 0, 4 or 8 (f32 layouts always have 4)                          */
+                        /* plan_wavefronts 0, 4 or 8                                                      */
   float *k_scale;       /* [B, Hkv, ceil(capacity / KEEPKV_QUANT_BLOCK)] scale of each block of K codes;  */
   float *v_scale;       /* and of V codes.  Those of blocks without a live slot mean nothing             */
 } keepkv_quant_cache;

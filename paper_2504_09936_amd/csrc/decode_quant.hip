@@ -24,14 +24,14 @@ int resident_quant(const keepkv_layout* L, long tiles_per_wave, int waves) {
 // takes the longer of one workgroup's rows (a compute unit pulls 36 GB/s, shared by its workgroups; a wavefront 25 GB/s, 19 in the tile loop) and of
 // all rows (6.2 TB/s); more rounds, smaller workgroups, a second tile, the loop and combining splits cost what stands below, in us.  The
 // constants are a fit to 7042 measured (shape, plan) pairs of 375 shapes (1 to 1024 heads, 64 to 32768 slots, head dims 64 and 128, groups of 1 to
-// 8), of which the plan chosen is 1.6 % slower than the best one (20 % at most).
+// 8), bf16, of which the plan chosen is 1.6 % slower than the best one (20 % at most); over 75 shapes of f32 it is 1.9 % (15 % at most).
 void choose_split_quant(const keepkv_layout* L, int capacity, long& per, int& waves) {
   const double units = (double)L->batch * L->n_kv_heads;
   const int group = L->n_q_heads / L->n_kv_heads;
   const double slot_bytes = 2.0 * L->head_dim + 20.0;
   const long max_ns = (capacity + kMinQuantSplit - 1) / kMinQuantSplit;
   double best = 1e300;
-  for (int wv = 4; wv <= (L->dtype == KEEPKV_F32 ? 4 : 8); wv += 4) {
+  for (int wv = 4; wv <= 8; wv += 4) {
     for (long ns = 1; ns <= max_ns && (ns == 1 || units * (double)ns <= kMaxQuantWorkgroups); ++ns) {
       long cand = ((capacity + ns - 1) / ns + kQBlock - 1) / kQBlock * kQBlock;
       if (cand < kMinQuantSplit) cand = kMinQuantSplit;
@@ -70,7 +70,6 @@ DecodePlan make_quant_plan(const keepkv_layout* L, int capacity, int force_per, 
   int waves = 4;
   choose_split_quant(L, capacity, per, waves);
   if (force_waves > 0) waves = force_waves;
-  if (L->dtype == KEEPKV_F32) waves = 4;
   if (force_per >= 64) per = force_per / kQBlock * kQBlock;
   long ns = (capacity + per - 1) / per;
   if (ns > 1024) { ns = 1024; per = ((capacity + ns - 1) / ns + 63) / 64 * 64; ns = (capacity + per - 1) / per; }
@@ -81,7 +80,7 @@ DecodePlan make_quant_plan(const keepkv_layout* L, int capacity, int force_per, 
   pl.bytes = decode_bytes(L, ns);
   // Splits that can meet within an XCD do, with one tile or two to a wavefront: against meeting through memory, over 90 shapes of 8 to 256 heads
   // and 256 to 8192 slots, the step takes 3 % less on average and 2 % more at worst, attention alone 2 % less and 5 % more.
-  const bool may_share = L->dtype == KEEPKV_BF16 && ns > 1 && ns <= kMaxLocalSplits && per <= 2L * waves * kQBlock && heads_fit_xcds(L);
+  const bool may_share = ns > 1 && ns <= kMaxLocalSplits && per <= (L->dtype == KEEPKV_BF16 ? 2L : 1L) * waves * kQBlock && heads_fit_xcds(L);
   pl.xcd_bytes = may_share ? decode_xcd_bytes(L, ns) : 0;
   return pl;
 }
@@ -136,7 +135,7 @@ size_t quant_workspace_bytes(const keepkv_layout* L, int capacity) {
   if (ns > kMaxQuantWorkgroups / units) ns = kMaxQuantWorkgroups / units;
   if (ns <= 1) return kWorkspaceHead;
   size_t bytes = decode_bytes(L, ns);
-  if (L->dtype == KEEPKV_BF16 && heads_fit_xcds(L) && decode_xcd_bytes(L, ns) > bytes) bytes = decode_xcd_bytes(L, ns);
+  if (heads_fit_xcds(L) && decode_xcd_bytes(L, ns) > bytes) bytes = decode_xcd_bytes(L, ns);
   return bytes;
 }
 

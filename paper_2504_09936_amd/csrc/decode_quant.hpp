@@ -567,13 +567,12 @@ keepkv_status launch_quant_g(const QuantParams& p, int units, bool step, hipStre
     return launch_status();
   };
   auto by_waves = [&](auto step_tag, auto tiles_tag, auto meet_tag) {
-    if constexpr (sizeof(T) == 2)                // (f32 layouts have four wavefronts, their queries take twice the room)
-      if (p.d.waves == 8) return go(step_tag, tiles_tag, meet_tag, std::integral_constant<int, 8>{});
+    if (p.d.waves == 8) return go(step_tag, tiles_tag, meet_tag, std::integral_constant<int, 8>{});
     return go(step_tag, tiles_tag, meet_tag, std::integral_constant<int, 4>{});
   };
   auto by_meet = [&](auto step_tag, auto tiles_tag) {
     if (p.d.nsplit == 1) return by_waves(step_tag, tiles_tag, std::integral_constant<int, kSoloMeet>{});
-    if constexpr (sizeof(T) == 2 && decltype(tiles_tag)::value != kLoop)
+    if constexpr (decltype(tiles_tag)::value != kLoop)
       if (p.d.arrivals != nullptr) return by_waves(step_tag, tiles_tag, std::integral_constant<int, kXcdMeet>{});
     return by_waves(step_tag, tiles_tag, std::integral_constant<int, kMemMeet>{});
   };
