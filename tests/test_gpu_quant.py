@@ -26,17 +26,14 @@ def check_head(c, b, h, want_k, want_v):
 
 
 # ------------------------------------------------------------------------------------------------ quantising, reading back
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("cap,more", [(1, 0), (31, 5), (32, 0), (33, 64), (100, 3), (513, 0)])
-def test_quantize_and_back(cap, more, D, dtype):
+def check_quantize_and_back(lens, cap, more, D, dtype):
     kk = U.kk()
     g = gen(cap * D)
-    lay = T.layout(2, 3, 2, D, dtype)
+    B, H = lens.shape
+    lay = T.layout(B, H, 2, D, dtype)
     src, dst = kk.Cache(lay, cap), kk.QuantCache(lay, cap + more)
     src.k.copy_(T.rows(g, src.k.shape, dtype, 8.0))
     src.v.copy_(T.rows(g, src.v.shape, dtype, 8.0) * 1e-3)
-    lens = torch.tensor([[0, 1, cap], [cap // 2, max(0, cap - 1), min(cap, 32)]], dtype=torch.int32)
     src.len.copy_(lens)
     src.votes.random_(1, 9, generator=g)
     src.log_s.normal_(generator=g)
@@ -51,14 +48,14 @@ def test_quantize_and_back(cap, more, D, dtype):
     kk.quantize(lay, src, dst)
     after = T.raw(dst)
     assert torch.equal(dst.len.cpu(), lens) and torch.equal(dst.t_obs, src.t_obs)
-    for b in range(2):
-        for h in range(3):
+    for b in range(B):
+        for h in range(H):
             n = int(lens[b, h])
             check_head(dst, b, h, Q.quantize(U.to_host(src.k)[b, h, :n]), Q.quantize(U.to_host(src.v)[b, h, :n]))
             for f in ("votes", "log_s", "born"):
                 assert torch.equal(getattr(dst, f)[b, h, :n], getattr(src, f)[b, h, :n]), f
             for f in ("k", "v", "votes", "log_s", "born", "k_scale", "v_scale"):                # what is dead stays
-                a, z = (x[f].view(2, 3, -1)[b, h] for x in (after, before))
+                a, z = (x[f].view(B, H, -1)[b, h] for x in (after, before))
                 live = -(-n // 32) if "scale" in f else n
                 per = a.numel() // (-(-(cap + more) // 32) if "scale" in f else cap + more)
                 assert torch.equal(a[live * per:], z[live * per:]), f
@@ -67,8 +64,8 @@ def test_quantize_and_back(cap, more, D, dtype):
         T.bits(getattr(back, f)).fill_(0x33)
     kk.dequantize(lay, dst, back)
     torch.cuda.synchronize()
-    for b in range(2):
-        for h in range(3):
+    for b in range(B):
+        for h in range(H):
             n = int(lens[b, h])
             (kc, ks), (vc, vs) = T.head(dst, b, h)
             np.testing.assert_array_equal(U.to_host(back.k)[b, h, :n], Q.values(kc, ks) if n else np.zeros((0, D)))
@@ -79,6 +76,22 @@ def test_quantize_and_back(cap, more, D, dtype):
                 rest = T.bits(getattr(back, f)[b, h, n:])
                 assert (rest == 0x33).all(), f
     assert torch.equal(back.len, src.len) and torch.equal(back.t_obs, src.t_obs)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("cap,more", [(1, 0), (31, 5), (32, 0), (33, 64), (100, 3), (513, 0)])
+def test_quantize_and_back(cap, more, D, dtype):
+    check_quantize_and_back(torch.tensor([[0, 1, cap], [cap // 2, max(0, cap - 1), min(cap, 32)]], dtype=torch.int32), cap, more, D, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_quantize_and_back_many_heads(D, dtype):
+    """More blocks than are read ahead of the lengths."""
+    lens = torch.randint(0, 301, (16, 8), generator=torch.Generator().manual_seed(D), dtype=torch.int32)
+    lens[0] = torch.tensor([0, 1, 31, 32, 33, 288, 299, 300])
+    check_quantize_and_back(lens, 300, 9, D, dtype)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
