@@ -235,31 +235,37 @@ struct AppendParams {
   int32_t* overflow;
   int n_tokens, capacity;
 };
-// live slots of a head, how many tokens are meant for it, how many fit
-__device__ __forceinline__ void append_range(const AppendParams& p, size_t unit, int& n, int& want, int& take) {
-  n = p.s.len[unit];
-  want = p.counts ? min(max(p.counts[unit], 0), p.n_tokens) : p.n_tokens;
-  take = min(want, p.capacity - n);
+// live slots of a head, its score updates, how many tokens are meant for it, how many fit
+struct Range {
+  int n, t_obs, want, take;
+};
+__device__ __forceinline__ Range append_range(const AppendParams& p, size_t unit) {
+  Range r;
+  r.n = p.s.len[unit];
+  r.t_obs = p.s.t_obs[unit];
+  r.want = p.counts ? min(max(p.counts[unit], 0), p.n_tokens) : p.n_tokens;
+  r.take = min(r.want, p.capacity - r.n);
+  return r;
 }
-__device__ __forceinline__ void append_move_on(const AppendParams& p, size_t unit, int n, int want, int take) {
-  if (take > 0) p.s.len[unit] = n + take;
-  if (take < want && p.overflow != nullptr) *p.overflow = 1;
+__device__ __forceinline__ void append_move_on(const AppendParams& p, size_t unit, const Range& r) {
+  if (r.take > 0) p.s.len[unit] = r.n + r.take;
+  if (r.take < r.want && p.overflow != nullptr) *p.overflow = 1;
 }
 // task 2 b + (0: K, 1: V): the b-th block that the tokens touch
 template <typename T, int D>
-__device__ __forceinline__ void append_task(const AppendParams& p, size_t unit, int task, int n, int take, int lane) {
+__device__ __forceinline__ void append_task(const AppendParams& p, size_t unit, int task, const Range& r, int lane) {
   const bool is_v = task & 1;
-  const int block = n / kQBlock + (task >> 1), base = block * kQBlock;
-  const int from = max(n, base), to = min(n + take, base + kQBlock);
+  const int block = r.n / kQBlock + (task >> 1), base = block * kQBlock;
+  const int from = max(r.n, base), to = min(r.n + r.take, base + kQBlock);
   if (from >= to) return;
-  const T* tokens = reinterpret_cast<const T*>(is_v ? p.v_t : p.k_t) + ((unit * p.n_tokens) + (from - n)) * D;
+  const T* tokens = reinterpret_cast<const T*>(is_v ? p.v_t : p.k_t) + ((unit * p.n_tokens) + (from - r.n)) * D;
   append_rows<T, D>(tokens, (is_v ? p.v : p.k) + unit * p.capacity * D, (is_v ? p.v_scale : p.k_scale) + unit * quant_blocks(p.capacity) + block,
                     block, from, to, lane);
   if (!is_v && from + lane < to) {
     const size_t at = unit * p.capacity + from + lane;
     p.s.votes[at] = 1;
     p.s.log_s[at] = -INFINITY;
-    p.s.born[at] = p.s.t_obs[unit];
+    p.s.born[at] = r.t_obs;
   }
 }
 
@@ -267,13 +273,12 @@ __device__ __forceinline__ void append_task(const AppendParams& p, size_t unit, 
 template <typename T, int D>
 __global__ __launch_bounds__(1024) void append_head_kernel(AppendParams p) {
   const size_t unit = blockIdx.x;
-  int n, want, take;
-  append_range(p, unit, n, want, take);
+  const Range r = append_range(p, unit);
   const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
-  const int tasks = take > 0 ? 2 * ((n + take - 1) / kQBlock - n / kQBlock + 1) : 0;
-  for (int task = threadIdx.x >> 6; task < tasks; task += waves) append_task<T, D>(p, unit, task, n, take, lane);
+  const int tasks = r.take > 0 ? 2 * ((r.n + r.take - 1) / kQBlock - r.n / kQBlock + 1) : 0;
+  for (int task = threadIdx.x >> 6; task < tasks; task += waves) append_task<T, D>(p, unit, task, r, lane);
   __syncthreads();
-  if (threadIdx.x == 0) append_move_on(p, unit, n, want, take);
+  if (threadIdx.x == 0) append_move_on(p, unit, r);
 }
 
 // Chunks of more tasks than a workgroup has wavefronts: a wavefront per task of all heads, and the lengths in a launch behind it.  One
@@ -284,16 +289,13 @@ template <typename T, int D>
 __global__ __launch_bounds__(kTaskWaves* kWave) void append_blocks_kernel(AppendParams p, int tasks) {
   const size_t unit = blockIdx.y;
   const int task = blockIdx.x * kTaskWaves + (threadIdx.x >> 6);
-  int n, want, take;
-  append_range(p, unit, n, want, take);
-  if (task < tasks && take > 0) append_task<T, D>(p, unit, task, n, take, threadIdx.x & 63);
+  const Range r = append_range(p, unit);
+  if (task < tasks && r.take > 0) append_task<T, D>(p, unit, task, r, threadIdx.x & 63);
 }
 __global__ __launch_bounds__(256) void append_lengths_kernel(AppendParams p, int units) {
   const int unit = blockIdx.x * 256 + threadIdx.x;
   if (unit >= units) return;
-  int n, want, take;
-  append_range(p, unit, n, want, take);
-  append_move_on(p, unit, n, want, take);
+  append_move_on(p, unit, append_range(p, unit));
 }
 
 bool rows_aligned(const keepkv_cache& c) { return aligned16(c.k) && aligned16(c.v); }
