@@ -14,7 +14,9 @@ namespace {
 
 // A wavefront owns tiles of 32 slots, which are the blocks that share a scale, and takes both products to the matrix cores (16x16x32,
 // bf16 operands): a code times its scale has 4 significant bits, so it is exact in bf16, and the conversion instruction applies the scale.
-// The query stays as it is (f32 queries as three bf16 terms, 24 bits) and products are summed in f32.
+// The query stays as it is (f32 queries as three bf16 terms, 24 bits) and products are summed in f32.  The weights of P V are two bf16
+// terms rounded to nearest (2^-18, where the output is rounded to 2^-9), of f32 layouts three (2^-27; with two an output was 1.6e-6 off, so
+// 1.3e-7, for 1 to 3 % of the time).
 //
 // K and V rows go to LDS by asynchronous copies of whole kilobytes.  (K rows loaded straight into the operand's registers, 64 bytes of a
 // row at a time, streamed 13 % slower: 221 MB in 40.9 us, 35.9 so.)  A K operand is read in an order of the channels that suits 16-byte
@@ -90,7 +92,7 @@ __global__ __launch_bounds__(kWaves* kWave, quant_waves_per_simd(sizeof(T), kTil
   constexpr int TILE_BYTES = kQBlock * D, BUFFER = 2 * TILE_BYTES, VLOADS = TILE_BYTES / (kWave * 16);
   constexpr int NV = kShare<G>;
   constexpr int WAVE_BYTES = quant_wave_bytes<T>(D, G, kTiles);
-  constexpr int QTERMS = kF32 ? 3 : 1;
+  constexpr int QTERMS = kF32 ? 3 : 1, PTERMS = kF32 ? 3 : 2;           // bf16 terms of a query element, of a weight
   constexpr int SCALARS = 2 + (STEP ? 1 : 0), REQUESTS = SCALARS + 2 * VLOADS;        // requests of a tile
   constexpr int EPL = D / kWave;                 // channels of a lane in an appended row
   extern __shared__ __align__(256) unsigned char smem_tiles[];
@@ -389,8 +391,19 @@ __global__ __launch_bounds__(kWaves* kWave, quant_waves_per_simd(sizeof(T), kTil
       __builtin_amdgcn_wave_barrier();
     }
     // ---- O += P V
-    uint32_t aw[2][4];
+    uint32_t aw[PTERMS][4];
     weights_operand<G, true>(pr, r_l, pos0, aw[0], aw[1]);
+    if constexpr (kF32) {                        // (and what two terms leave)
+      float rest[NV];
+      uint32_t none[4];
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        auto nearest = [](float x) { return bf16_to_f32(f32_to_bf16_bits(x)); };
+        rest[v] = pr[v] - nearest(pr[v]);
+        rest[v] -= nearest(rest[v]);
+      }
+      weights_operand<G, true>(rest, r_l, pos0, aw[2], none);
+    }
     const int vrow = 16 * (l16 >> 3) + 4 * q + ((l16 >> 1) & 3);      // the row whose half this lane's address names
     typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
     u32x2_t b[NTILE];
@@ -416,7 +429,7 @@ __global__ __launch_bounds__(kWaves* kWave, quant_waves_per_simd(sizeof(T), kTil
           : "memory");
     v_done();
 #pragma unroll
-    for (int part = 0; part < 2; ++part)
+    for (int part = 0; part < PTERMS; ++part)
 #pragma unroll
       for (int nt = 0; nt < NTILE; ++nt)
         O[nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, make_uint4(aw[part][0], aw[part][1], aw[part][2], aw[part][3])),

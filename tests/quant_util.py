@@ -89,12 +89,12 @@ def attention(c, lay, q, b, h):
     With A = scale * sum_d |q_d k_d| at most over slots and heads, a logit is a sum of D exact products (D half steps of A), times
     the scales (3 more); so a weight and the sum of weights are each off by a factor within e^+-d, d = (D + 4) A EPS32 + |z| EPS32 for
     adding ln p and subtracting the maximum (|z| <= A + ln p), and the hardware's exp2 and log2 (2^-22 and, of ln p, 2^-22 of it).
-    P is held in two bf16 terms (2^-16), sums over n slots in f32 add n half steps: in all an output is off by at most
-    w = 2 d + 2^-16 + 2^-21 + (n + 16) EPS32 times sum_i w_i |v_i|, before it is rounded to its type.
+    P is held in bf16 terms, two (2^-16) or, f32 layouts, three (2^-24), sums over n slots in f32 add n half steps: in all an output is off
+    by at most w = 2 d + 2^-16 (2^-24) + 2^-21 + (n + 16) EPS32 times sum_i w_i |v_i|, before it is rounded to its type.
 
     Beside that, where all weights but one are below 2^-100: the 16 rows of the matrix product hold each head 16 / G times, a slot's
-    weight in one of them and the smallest normal number, not zero, in the others, in each of the two terms; a tile's sum is scaled by
-    at most 1 and divided by a sum of weights of at least 1.  So (16 / G - 1) * 2 * 2^-126 * sum_i |v_i| at most is added."""
+    weight in one of them and the smallest normal number, not zero, in the others, in each of the terms; a tile's sum is scaled by
+    at most 1 and divided by a sum of weights of at least 1.  So (16 / G - 1) * 2 (3) * 2^-126 * sum_i |v_i| at most is added."""
     G, D = lay.n_q_heads // lay.n_kv_heads, lay.head_dim
     (kc, ks), (vc, vs) = head(c, b, h)
     n = len(kc)
@@ -108,11 +108,11 @@ def attention(c, lay, q, b, h):
     A = scale * (np.abs(qh)[:, None, :] * np.abs(K)[None]).sum(-1).max()
     lp = np.log(votes.max())
     d = (D + 4) * A * EPS32 + 4 * (A + lp) * EPS32 + lp * 2.0 ** -22
-    w = 2 * d + 2.0 ** -16 + 2.0 ** -21 + (n + 16) * EPS32
+    w = 2 * d + 2.0 ** (-16 if lay.dtype == U.kk().BF16 else -24) + 2.0 ** -21 + (n + 16) * EPS32
     z = scale * qh @ K.T + np.log(votes)
     p = np.exp(z - lse[:, None])
     half = 2.0 ** -8 if lay.dtype == U.kk().BF16 else EPS32
-    e_out = half * np.abs(out) * (1 + w) + w * (p @ np.abs(V)) + (16 // G - 1) * 2.0 ** -125 * (1 + half) * np.abs(V).sum(0) + 1e-38
+    e_out = half * np.abs(out) * (1 + w) + w * (p @ np.abs(V)) + (16 // G - 1) * (2 if lay.dtype == U.kk().BF16 else 3) * 2.0 ** -126 * (1 + half) * np.abs(V).sum(0) + 1e-38
     return (out, lse, mean), (e_out, d + (n + 16) * EPS32 + 2.0 ** -22 + np.abs(lse) * 4 * EPS32, np.full(n, (D + 6) * A * EPS32))
 
 
