@@ -127,7 +127,8 @@ keepkv_status keepkv_append(const keepkv_layout *layout, keepkv_cache *cache,
  * the G query heads of the group of scale*q.k_i = ln s_i of the group-mean query (the
  * score keepkv_score consumes).  lse_out (DEVICE f32 [B, Hq], may be NULL): ln sum_i p_i s_i.
  * An empty cache (len == 0) gives out = 0 and lse = -inf.  Dead slots are never read.
- * Needs workspace (split partial results). */
+ * A key that holds a NaN, a query that is not finite or a logit beyond f32 makes NaN of out and lse of the query heads that it reaches, and of no
+ * others.  Needs workspace (split partial results). */
 keepkv_status keepkv_decode_attn(const keepkv_layout *layout, const keepkv_cache *cache,
                                  const void *q, void *out, float *logits_out, float *lse_out,
                                  void *workspace, size_t workspace_bytes, void *stream);

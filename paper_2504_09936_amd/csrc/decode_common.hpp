@@ -343,12 +343,12 @@ __device__ __forceinline__ void combine_and_finish(const DecodeParams& p, const 
   auto finish = [&](int idx, float M, float L, float A) {
     const int g = head_of(idx), d = kInner ? idx / G : idx % D;
     const size_t row = (size_t)unit * G + g;   // == b * Hq + h * G + g
-    const float o = (L > 0.f) ? A / L : 0.f;
+    const float o = L == 0.f ? 0.f : A / L;      // (no slot, or none of any weight: zero; a sum that is NaN shows as one)
     if constexpr (kBf16)
       reinterpret_cast<uint16_t*>(p.out)[row * D + d] = (uint16_t)f32_to_bf16_bits(o);
     else
       reinterpret_cast<float*>(p.out)[row * D + d] = o;
-    if (d == 0 && p.lse_out != nullptr) p.lse_out[row] = (L > 0.f) ? (M + fast_log2(L)) * kLn2 : -INFINITY;
+    if (d == 0 && p.lse_out != nullptr) p.lse_out[row] = L == 0.f ? -INFINITY : (M + fast_log2(L)) * kLn2;
   };
 
   float* const partials = p.partial + (size_t)unit * p.nsplit * p.split_stride;   // this head's splits
