@@ -128,7 +128,8 @@ keepkv_status keepkv_append(const keepkv_layout *layout, keepkv_cache *cache,
  * score keepkv_score consumes).  lse_out (DEVICE f32 [B, Hq], may be NULL): ln sum_i p_i s_i.
  * An empty cache (len == 0) gives out = 0 and lse = -inf.  Dead slots are never read.
  * A key that holds a NaN, a query that is not finite or a logit beyond f32 makes NaN of out and lse of the query heads that it reaches, and of no
- * others.  Needs workspace (split partial results). */
+ * others.  Of a bf16 cache, values of weight zero may add up to (16/G - 1) * 2^-125 times the sum of their magnitudes to an output, which only
+ * values of 1e30 and more make visible.  Needs workspace (split partial results). */
 keepkv_status keepkv_decode_attn(const keepkv_layout *layout, const keepkv_cache *cache,
                                  const void *q, void *out, float *logits_out, float *lse_out,
                                  void *workspace, size_t workspace_bytes, void *stream);
@@ -298,7 +299,7 @@ keepkv_status keepkv_prefill_merge(const keepkv_layout *layout, const keepkv_cac
  * finite becomes NaN.  Since a scale is a power of two, dividing by it rounds nothing, reading back is exact (in f32 and in
  * bf16), and rows that were read back are quantised again to the same values except where those become subnormal under a
  * larger scale (a value below 2^-6 of the scale keeps multiples of 2^-9 of it).  Numbers within 2^-4 of the largest f32 may
- * round to 2^128, which reads back as infinity.  Scales are read by their exponent: caches hold what these calls have written.
+ * round to 2^128, which reads back as infinity (and, attended to, makes NaN of what it reaches).  Scales are read by their exponent: caches hold what these calls have written.
  * Half the bytes of a bf16 cache, and its decode calls read them as they are. */
 #define KEEPKV_QUANT_BLOCK 32
 
@@ -335,7 +336,8 @@ keepkv_status keepkv_append_quant(const keepkv_layout *layout, keepkv_quant_cach
                                   const int32_t *counts, int32_t *overflow, void *stream);
 
 /* keepkv_decode_attn on a cache of codes: Eq. 6 over the values code * scale, with the same arguments (q and out in the layout's
- * dtype, f32 or bf16) and the same treatment of empty and dead slots.  Products of q and codes are exact, sums f32. */
+ * dtype, f32 or bf16) and the same treatment of empty and dead slots.  Products of q and codes are exact, sums f32 (values or logits whose
+ * sums f32 does not hold become infinities and NaN). */
 keepkv_status keepkv_decode_attn_quant(const keepkv_layout *layout, const keepkv_quant_cache *cache,
                                        const void *q, void *out, float *logits_out, float *lse_out,
                                        void *workspace, size_t workspace_bytes, void *stream);

@@ -224,14 +224,15 @@ __device__ __forceinline__ void take_shares(const f32x4_t (&s)[2], int r_l, int 
   }
 }
 
-// The weights of a lane share as the A operand of O = P V, hi + lo in bf16 (16 significant bits).  The places of the slots that
-// other lanes took hold the smallest normal number and not zero: against any finite V it vanishes beside the head's largest weight (1),
-// and an infinity in V stays one, where zero would make it a NaN.  Each term is cut off (together within 2^-15 of the weight) or,
-// kNearest, rounded (2^-18).
+// The weights of a lane share as the A operand of O = P V, hi + lo in bf16 (16 significant bits).  Each term is cut off (together within
+// 2^-15 of the weight) or, kNearest, rounded (2^-18).  The places of the slots that other lanes took hold zero where V is made of codes
+// (kNearest).  Where V is made of bf16 rows they hold the smallest normal number: an infinite value then stays infinite where the weight has both
+// terms, and zero would always make it NaN; finite values add up to (16 / G - 1) 2^-125 sum |v| to an output (8 for G = 8 and
+// one value near the largest f32).
 template <int G, bool kNearest>
 __device__ __forceinline__ void weights_operand(const float (&pr)[kShare<G>], int r_l, int pos0, uint32_t (&ah)[4], uint32_t (&al)[4]) {
   constexpr int NV = kShare<G>;
-  constexpr uint32_t kNone = 0x00800080u;
+  constexpr uint32_t kNone = kNearest ? 0u : 0x00800080u;
   if constexpr (NV == 1) {
     const uint32_t hb = kNearest ? f32_to_bf16_bits(pr[0]) << 16 : __builtin_bit_cast(uint32_t, pr[0]) & 0xFFFF0000u;
     const float rest = pr[0] - __builtin_bit_cast(float, hb);
