@@ -562,7 +562,7 @@ __device__ __forceinline__ void combine_and_finish(const DecodeParams& p, const 
 
 // ---- plans (host) ----------------------------------------------------------------------------------------------
 inline size_t decode_bytes(const keepkv_layout* L, long nsplit) {
-  return kWorkspaceHead + align_up((size_t)L->batch * L->n_q_heads * nsplit * (L->head_dim + 2) * sizeof(float), 256);
+  return kWorkspaceHead + (size_t)L->batch * L->n_q_heads * nsplit * (L->head_dim + 2) * sizeof(float);
 }
 
 // Partial results with cache lines of their own, for heads that are combined within an XCD.
