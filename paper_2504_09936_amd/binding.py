@@ -132,14 +132,18 @@ _HOT_QUANT = ("decode_step_quant", "decode_attn_quant", "append_quant", "quantiz
 try:
     from . import _pycall
 except ImportError:
-    _fast = dict.fromkeys(_HOT)
-    _fast_quant = dict.fromkeys(_HOT_QUANT)
-else:
-    _fast_quant = dict(zip(_HOT_QUANT, _pycall.bind_quant(_raw_stream, _device, C.ArgumentError,
-                                                          *(C.cast(getattr(_lib, "keepkv_" + f), C.c_void_p).value
-                                                            for f in _HOT_QUANT))))
-    _fast = dict(zip(_HOT, _pycall.bind(_raw_stream, _device, C.ArgumentError,
-                                        *(C.cast(getattr(_lib, "keepkv_" + f), C.c_void_p).value for f in _HOT))))
+    _pycall = None
+
+
+def _bound(names, bind: str) -> dict:
+    """The extension's functions of this library's calls, None for each where there is no extension, or one built before it had them."""
+    if not hasattr(_pycall, bind):
+        return dict.fromkeys(names)
+    return dict(zip(names, getattr(_pycall, bind)(_raw_stream, _device, C.ArgumentError,
+                                                  *(C.cast(getattr(_lib, "keepkv_" + f), C.c_void_p).value for f in names))))
+
+
+_fast, _fast_quant = _bound(_HOT, "bind"), _bound(_HOT_QUANT, "bind_quant")
 
 
 def _fast_call(name: str, layout, cache):
