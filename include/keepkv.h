@@ -299,8 +299,8 @@ keepkv_status keepkv_prefill_merge(const keepkv_layout *layout, const keepkv_cac
  * finite becomes NaN.  Since a scale is a power of two, dividing by it rounds nothing, reading back is exact (in f32 and in
  * bf16), and rows that were read back are quantised again to the same values except where those become subnormal under a
  * larger scale (a value below 2^-6 of the scale keeps multiples of 2^-9 of it).  Numbers within 2^-4 of the largest f32 may
- * round to 2^128, which reads back as infinity (and, attended to, makes NaN of what it reaches).  Scales are read by their exponent: caches hold what these calls have written.
- * Half the bytes of a bf16 cache, and its decode calls read them as they are. */
+ * round to 2^128, which reads back as infinity (and, attended to, makes NaN of what it reaches).  Scales are read by their exponent:
+ * caches hold what these calls have written.  Half the bytes of a bf16 cache, and its decode calls read them as they are. */
 #define KEEPKV_QUANT_BLOCK 32
 
 /* One layer's cache of codes (HOST struct of DEVICE pointers, caller-owned).  The calls that read no rows take &cache->c as their
@@ -330,6 +330,7 @@ keepkv_status keepkv_dequantize(const keepkv_layout *layout, const keepkv_quant_
  * `overflow` (DEVICE int32, may be NULL) is set to 1 if some did not fit.  A block that held live slots before keeps its scale unless
  * the new rows need a larger one, s' : then its live codes become rne(code * s / s'), a shift of exponents that is exact
  * except where a code becomes subnormal.  A block whose first slot is among the new ones starts with the scale that they need.
+ * Lowering len takes tokens off again, but not the scales that they made grow: codes that became subnormal for such a token stay so.
  * n_tokens >= 1.  Needs no workspace. */
 keepkv_status keepkv_append_quant(const keepkv_layout *layout, keepkv_quant_cache *cache,
                                   const void *k_t, const void *v_t, int32_t n_tokens,

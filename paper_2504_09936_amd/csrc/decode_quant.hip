@@ -9,7 +9,8 @@ namespace {
 constexpr int kMaxQuantWorkgroups = 512;         // that share heads: bounds the workspace
 constexpr int kMinQuantSplit = 64;
 
-// Workgroups that a compute unit holds: by LDS (K and V tiles and the query rows, once per wavefront or, the loop's, once) and registers.
+// Workgroups that a compute unit holds: by LDS (K and V tiles and the query rows, once per wavefront or, the loop's, once) and registers.  (As the
+// bf16 kernels are: two tiles of an f32 layout run as the loop, whose registers leave room for twelve wavefronts.)
 int resident_quant(const keepkv_layout* L, long tiles_per_wave, int waves) {
   const bool f32 = L->dtype == KEEPKV_F32, loop = tiles_per_wave > 2;
   const int rows = (tiles_per_wave == 2 ? 4 : 2) * kQBlock * L->head_dim;
@@ -24,7 +25,9 @@ int resident_quant(const keepkv_layout* L, long tiles_per_wave, int waves) {
 // takes the longer of one workgroup's rows (a compute unit pulls 36 GB/s, shared by its workgroups; a wavefront 25 GB/s, 19 in the tile loop) and of
 // all rows (6.2 TB/s); more rounds, smaller workgroups, a second tile, the loop and combining splits cost what stands below, in us.  The
 // constants are a fit to 7042 measured (shape, plan) pairs of 375 shapes (1 to 1024 heads, 64 to 32768 slots, head dims 64 and 128, groups of 1 to
-// 8), bf16, of which the plan chosen is 1.6 % slower than the best one (20 % at most); over 75 shapes of f32 it is 1.9 % (15 % at most).
+// 8), bf16, of which the plan chosen is 1.6 % slower than the best one (20 % at most); over 75 shapes of f32 it is 1.9 % (15 % at most).  Two
+// things that it does not see: the next split's tiles, which a two-tile launch reads where its own has fewer (64 heads x 1180 slots: four splits of ten
+// tiles on eight wavefronts), and whether splits may meet within an XCD.
 void choose_split_quant(const keepkv_layout* L, int capacity, long& per, int& waves) {
   const double units = (double)L->batch * L->n_kv_heads;
   const int group = L->n_q_heads / L->n_kv_heads;

@@ -471,7 +471,7 @@ __global__ __launch_bounds__(kWaves* kWave, quant_waves_per_simd(sizeof(T), kTil
   } else if constexpr (kTiles == kTwo) {
     if (base < lim) {
       request(base, t0, Tb);
-      request(base + kTileStep, t1, Tb + BUFFER);                     // (beyond the last row its copies bring zeros)
+      request(base + kTileStep, t1, Tb + BUFFER);                     // (beyond the head's last row zeros, beyond the split the next one's rows)
       read_new();
       await(kTwoTiles);
       read_q();
